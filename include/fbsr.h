@@ -81,6 +81,10 @@ typedef enum {
  * the other entry points, and calls whose pointers are off the fast path's alignment, use the general kernel. */
 #define FBSR_OVF_IEEE 0x100
 
+/* binary32, for the arguments that name the type of a SOURCE (g_fmt of fbsr_adamw_multi, src_fmt of fbsr_round_w4, out_fmt
+ * of fbsr_gemv_w4); it is not a target of rounding. */
+#define FBSR_FP32 0x20
+
 /* Round-up predicates: the few-bit stochastic ones of Section II-B and Eq. (8), and the deterministic
  * ones of Section II-A (ties to even, ties away from zero (Eq. (4)), ties to odd), which use no draw:
  * for those k_bits, seed and offset are ignored (k_bits must still be in 1..16). */
@@ -282,6 +286,47 @@ int fbsr_accumulate(void* w_lp, const float* update, size_t n, int fmt, int vari
 int fbsr_qat_adamw_step(void* w8, const void* grad16, float* m, float* v, size_t n, int w_fmt, int g_fmt, int variant,
                         int k_bits, uint64_t seed, uint64_t offset, float lr, float beta1, float beta2, float eps,
                         float weight_decay, int step, void* cuda_stream);
+
+/* fbsr_adamw_multi -- Algorithm 1's AdamW update of a whole model: one step over `count` tensors, with the moments in
+ * binary32 or in 8 bits, and the SR write of each tensor's low-precision copy.  Per element, binary32, every operation
+ * rounded once; the host scalars c1, c2, a1, a2 (as in fbsr_adam_update) and decay = 1 - lr weight_decay are formed in
+ * binary64 from the binary64 arguments and then rounded to binary32, as beta1, beta2 and eps are:
+ *     g = fl(value(g) grad_scale);  m' = fma(beta1, m, a1 g);  v' = fma(beta2, v, (a2 g) g);  r = sqrt(v');
+ *     w' = fma(-c1, m' / fl(fl(r c2) + eps), fl(w decay));  w_lp = FBSR(w')
+ * With weight_decay = 0, binary32 gradients and state, no grad_scale and scalars that are binary32 numbers, every
+ * tensor's result is that of fbsr_adam_update with its `offset`, bit for bit.
+ *   tensors     HOST array, read before the call returns; a tensor with n = 0 is skipped.  Tensors must not overlap.
+ *     w           device, n binary32 master weights, updated in place
+ *     g           device, n gradients of g_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16), read only
+ *     m, v        device: n binary32 moments (state_bits 32), or n codes (state_bits 8), updated in place
+ *     m_scale, v_scale   state_bits 8: device, ceil(n / 256) binary32 scales each, updated in place; else ignored
+ *     w_lp        device, n codes of `fmt`, overwritten; NULL: no copy of this tensor is written
+ *     offset      global index of the tensor's element 0 for the draws; a multiple of 256
+ *   grad_scale  device, one binary32 factor (loss unscaling, clipping) read when the kernel runs; NULL = 1
+ * 8-bit state: 256 consecutive elements of a tensor share a scale.  m holds E4M3 codes of m' / s, v holds E4M3 codes of
+ * sqrt(v') / s, s = max(fl(amax fl(1 / 448)), 2^-126) with amax the block's largest finite magnitude of what is stored;
+ * products and sums of m' and v' are rounded one by one here (no fma), so that plain binary32 arithmetic reproduces codes:
+ *     code = FBSR_E4M3(fl(x fl(1 / s))), the same variant and k_bits as the weights; a root above zero whose code came out
+ *     as zero takes the smallest code, so that a moment never vanishes under a step that divides by it.
+ * Fresh state is all zeros, scales included.  The draws of element J = offset + j for the two states are bits [0, k) and
+ * [8, 8 + k) of halfword J mod 8 (low half of word 0 first) of the generator call with counter (J / 8 lo, hi, 1, 0); the
+ * weights draw from counters (.., .., 0, 0) as everywhere else.  Stochastic variants need k_bits <= 8 with 8-bit state
+ * (FBSR_ERR_UNSUPPORTED).  Every 400 tensors cost one launch.  Any element alignment is accepted; tensors whose pointers
+ * allow it (32 bytes for binary32, 16 for 16-bit, 8 for 8-bit arrays) are read and written eight elements at a time. */
+typedef struct {
+    float* w;
+    const void* g;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* w_lp;
+    uint64_t n, offset;
+} fbsr_adamw_tensor;
+
+int fbsr_adamw_multi(const fbsr_adamw_tensor* tensors, size_t count, int state_bits, int g_fmt, int fmt, int variant,
+                     int k_bits, uint64_t seed, double lr, double beta1, double beta2, double eps, double weight_decay,
+                     int step, const float* grad_scale, void* cuda_stream);
 
 /* fbsr_qat_update -- Algorithm 1, last line, with the sum formed in the 16-bit format as written there:
  *     w16 = value(w8);  s = RTNE_16(fl32(w16 + u16));  w8 = FBSR(s)          (in place on w8)

@@ -14,6 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfbsr.so")
 
 FMT = {"bf16": 0, "fp16": 1, "e4m3": 2, "e5m2": 3, "b8p4": 4}
+FP32 = 0x20               # FBSR_FP32: names binary32 where a source may have several types
 OVF_IEEE = 0x100          # or into a format id, or append "+ieee" to a format name: IEEE overflow instead of saturation
 VARIANT = {"srff": 0, "srf": 1, "src": 2, "rtne": 3, "rta": 4, "rto": 5}
 CODE_DTYPE = {"bf16": torch.uint16, "fp16": torch.uint16, "e4m3": torch.uint8, "e5m2": torch.uint8, "b8p4": torch.uint8}
@@ -40,6 +41,13 @@ class FbsrFormatDesc(ctypes.Structure):
                 ("single_zero", ctypes.c_int32)]
 
 
+class FbsrAdamwTensor(ctypes.Structure):
+    """fbsr_adamw_tensor of include/fbsr.h."""
+    _fields_ = [("w", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("w_lp", ctypes.c_void_p),
+                ("n", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
+
+
 def format_desc(K, P, B, max_code, inf_code=None, nan_code=0, single_zero=False):
     """Fill in an FbsrFormatDesc; inf_code=None means that the format has no infinity."""
     return FbsrFormatDesc(K, P, B, max_code, 0 if inf_code is None else 1, 0 if inf_code is None else inf_code,
@@ -52,6 +60,7 @@ def _load():
                           "(there is no fallback implementation)")
     L = ctypes.CDLL(_LIB_PATH)
     vp, sz, i, u64, f = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint64, ctypes.c_float
+    d = ctypes.c_double
     L.fbsr_round.argtypes = [vp, vp, sz, i, i, i, u64, u64, f, vp]
     L.fbsr_round_bits.argtypes = [vp, vp, sz, i, i, i, vp, f, vp]
     L.fbsr_round_mx.argtypes = [vp, vp, vp, sz, i, i, i, u64, u64, vp]
@@ -74,6 +83,8 @@ def _load():
     L.fbsr_qat_update.restype = i
     L.fbsr_qat_adamw_step.argtypes = [vp, vp, vp, vp, sz, i, i, i, i, u64, u64, f, f, f, f, f, i, vp]
     L.fbsr_qat_adamw_step.restype = i
+    L.fbsr_adamw_multi.argtypes = [ctypes.POINTER(FbsrAdamwTensor), sz, i, i, i, i, i, u64, d, d, d, d, d, i, vp, vp]
+    L.fbsr_adamw_multi.restype = i
     L.fbsr_round_host_min_workspace.argtypes = []
     L.fbsr_round_host_min_workspace.restype = sz
     L.fbsr_round_host.argtypes = [vp, vp, sz, i, i, i, u64, u64, f, vp, sz, vp]
@@ -324,6 +335,90 @@ def fbsr_qat_adamw_step(w8, grad16, m, v, w_fmt, g_fmt, variant, k_bits, seed, o
                                       _fmt(g_fmt), _var(variant), k_bits, seed, offset, lr, beta1, beta2, eps, weight_decay,
                                       step, _stream(w8)), "fbsr_qat_adamw_step")
     return w8
+
+
+ADAMW_BLOCK = 256         # elements that share a scale of the 8-bit state
+SOURCE_TYPE = {torch.float32: FP32, torch.bfloat16: FMT["bf16"], torch.float16: FMT["fp16"]}
+
+
+class FbsrAdamwTensors:
+    """The tensors of one fbsr_adamw_multi call: lists of equal length, one entry per tensor.
+
+    w: float32 masters; g: gradients, all float32, all bfloat16 or all float16; m, v: float32 moments, or 8-bit codes
+    (uint8 or float8_e4m3fn) with m_scale, v_scale (float32, one per 256 elements); lp: the low-precision copies (codes
+    of `fmt`, or a tensor of the torch dtype of that format), with None for tensors that have none, or None for all.
+    offsets: the tensors' places in the stream of random draws, multiples of 256; by default each tensor starts at the
+    next multiple of 256 after the previous one.  Holds references to the tensors; set_grads() exchanges the gradients."""
+
+    def __init__(self, w, g, m, v, lp=None, fmt="bf16", m_scale=None, v_scale=None, offsets=None):
+        count = len(w)
+        if offsets is None:
+            offsets, at = [], 0
+            for t in w:
+                offsets.append(at)
+                at += -(-t.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
+        if lp is None:
+            lp = [None] * count
+        if (m_scale is None) != (v_scale is None):
+            raise ValueError("m_scale and v_scale belong together")
+        self.state_bits = 32 if m_scale is None else 8
+        if m_scale is None:
+            m_scale = v_scale = [None] * count
+        for what, x in (("g", g), ("m", m), ("v", v), ("lp", lp), ("m_scale", m_scale), ("v_scale", v_scale), ("offsets", offsets)):
+            if len(x) != count:
+                raise ValueError("%s has %d entries for %d tensors" % (what, len(x), count))
+        self.fmt, self.device = fmt, w[0].device if count else None
+        self.array = (FbsrAdamwTensor * max(count, 1))()
+        self.count = count
+        self._w, self._state, self._lp = list(w), (list(m), list(v), list(m_scale), list(v_scale)), list(lp)
+        state = (torch.float32,) if self.state_bits == 32 else (torch.uint8, torch.float8_e4m3fn)
+        code = (CODE_DTYPE[_fmt_name(fmt)],) + ((VIEW_DTYPE[_fmt_name(fmt)],) if _fmt_name(fmt) in VIEW_DTYPE else ())
+        for i in range(count):
+            n, d = w[i].numel(), self.array[i]
+            blocks = -(-n // ADAMW_BLOCK)
+            d.w = self._pointer(w[i], n, (torch.float32,), "w", i)
+            d.m = self._pointer(m[i], n, state, "m", i)
+            d.v = self._pointer(v[i], n, state, "v", i)
+            if self.state_bits == 8:
+                d.m_scale = self._pointer(m_scale[i], blocks, (torch.float32,), "m_scale", i)
+                d.v_scale = self._pointer(v_scale[i], blocks, (torch.float32,), "v_scale", i)
+            d.w_lp = None if lp[i] is None else self._pointer(lp[i], n, code, "lp", i)
+            d.n, d.offset = n, int(offsets[i])
+        self.set_grads(g)
+
+    def _pointer(self, t, n, dtypes, what, i):
+        if not (t.is_cuda and t.device == self.device and t.is_contiguous() and t.dtype in dtypes):
+            raise TypeError("%s[%d] must be a contiguous tensor of %s on %s" % (what, i, " or ".join(map(str, dtypes)), self.device))
+        if t.numel() != n:
+            raise ValueError("%s[%d] has %d elements, expected %d" % (what, i, t.numel(), n))
+        return t.data_ptr()
+
+    def set_grads(self, g):
+        if len(g) != self.count:
+            raise ValueError("g has %d entries for %d tensors" % (len(g), self.count))
+        dtype = g[0].dtype if self.count else torch.float32
+        if dtype not in SOURCE_TYPE:
+            raise TypeError("gradients must be float32, bfloat16 or float16")
+        pointers = [self._pointer(t, self._w[i].numel(), (dtype,), "g", i) for i, t in enumerate(g)]
+        for d, p in zip(self.array, pointers):
+            d.g = p
+        self.g_fmt, self._g = SOURCE_TYPE[dtype], list(g)
+
+
+def fbsr_adamw_multi(tensors, variant, k_bits, seed, lr, beta1, beta2, eps, weight_decay, step, grad_scale=None):
+    """One AdamW step over all tensors of an FbsrAdamwTensors, in place.  grad_scale: a one-element float32 CUDA tensor."""
+    if tensors.count == 0:
+        return tensors
+    gs = None
+    if grad_scale is not None:
+        if grad_scale.numel() != 1 or grad_scale.device != tensors.device:
+            raise ValueError("grad_scale must be one element on %s" % tensors.device)
+        gs = _dev(grad_scale, torch.float32, "grad_scale")
+    with torch.cuda.device(tensors.device):
+        _check(_L.fbsr_adamw_multi(tensors.array, tensors.count, tensors.state_bits, tensors.g_fmt, _fmt(tensors.fmt),
+                                   _var(variant), k_bits, seed, lr, beta1, beta2, eps, weight_decay, step, gs,
+                                   _stream(tensors._w[0])), "fbsr_adamw_multi")
+    return tensors
 
 
 def fbsr_round_host(src_host, dst_host, fmt, variant, k_bits, seed, offset, scale, workspace):

@@ -20,9 +20,11 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std
          "-Xcompiler", "-fPIC", "-Xcompiler", "-O2", "--fmad=false"]
 HEADERS = ["fbsr_device.cuh", "fbsr_kernels.cuh", "fbsr_internal.h", os.path.join("..", "..", "include", "fbsr.h")]
 
+SINGLE_UNITS = ["fbsr_api", "fbsr_descriptor", "fbsr_adamw_multi"]      # sources compiled once, as they are
+
 
 def _units():
-    units = [("fbsr_api.o", "fbsr_api.cu", []), ("fbsr_descriptor.o", "fbsr_descriptor.cu", [])]
+    units = [(name + ".o", name + ".cu", []) for name in SINGLE_UNITS]
     for group in (2, 6, 5, 3, 1, 0, 4):       # the longest compilations first
         for fmt in range(5):
             if group in (2, 3, 6) and fmt < 2:
@@ -33,9 +35,8 @@ def _units():
 
 
 def _newest_source():
-    paths = [os.path.join(CSRC, h) for h in HEADERS] + [os.path.join(CSRC, "fbsr_api.cu"),
-                                                        os.path.join(CSRC, "fbsr_dispatch.cu"),
-                                                        os.path.join(CSRC, "fbsr_descriptor.cu"), __file__]
+    sources = [name + ".cu" for name in SINGLE_UNITS] + ["fbsr_dispatch.cu"]
+    paths = [os.path.join(CSRC, f) for f in HEADERS + sources] + [__file__]
     return max(os.path.getmtime(p) for p in paths)
 
 
