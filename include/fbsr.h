@@ -178,6 +178,31 @@ int fbsr_format_desc_valid(const fbsr_format_desc* desc);
 int fbsr_round_mx(const float* src, void* dst, uint8_t* scales, size_t n, int fmt, int variant, int k_bits,
                   uint64_t seed, uint64_t offset, void* cuda_stream);
 
+/* fbsr_round_w4 -- block-scaled rounding of a weight matrix to 4 bits (Section I-A's scaled values; the target is E2M1 =
+ * (K, P, B; M) = (4, 2, 1; 6): 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign).  `group` (32, 64 or 128) consecutive elements of a
+ * row share a scale s; with amax the group's largest finite magnitude (0 if none):
+ *     FBSR_SCALE_E8M0  s = 2^e, e = max(floor(log2 amax) - 2, -127) (-127 if amax < 2^-126): one byte e + 127.  As in
+ *                      fbsr_round_mx, the maximum lands in the top binade and what exceeds 6 s saturates.
+ *     FBSR_SCALE_BF16  s = fl(amax fl(1 / 6)) rounded up to bfloat16, at least 2^-126, at most the largest bfloat16 whose
+ *                      sixfold is finite in the source's type; stored as that bfloat16.
+ *     code = FBSR_E2M1(fl(x fl(1 / s)));  value = code s.   Infinities saturate.  A group that holds a NaN gets the NaN scale
+ *     (byte 255, or bfloat16 0x7FC0) and zero codes: all of it reads as NaN.
+ *   src        device, rows x cols values of src_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16), row r at src + r src_ld (elements)
+ *   codes      device, rows x (padded / 2) bytes, padded = fbsr_w4_padded(cols): cols rounded up to a multiple of 128, the
+ *              rest filled with zeros; 16-byte aligned.  A 32-bit word holds 8 consecutive elements, the first in its lowest
+ *              bits; in every 64 bytes (128 elements) word 4 j + t of plain order lies at place 4 t + j (j, t = 0..3).
+ *   scales     device, rows x (padded / group) bytes or bfloat16
+ *   values     NULL, or device, rows x cols of src_fmt at values + r values_ld: the values that the codes stand for, rounded
+ *              once to src_fmt (what a forward pass over 4-bit weights multiplies with); must not overlap src
+ *   offset     a multiple of 128, at most 2^62; element (r, c) has the global index offset + r padded + c for its draw.
+ * Rows whose addresses allow it (32 bytes for binary32, 16 for 16-bit) are read and written eight elements at a time. */
+#define FBSR_SCALE_E8M0 0
+#define FBSR_SCALE_BF16 1
+size_t fbsr_w4_padded(size_t cols);
+int fbsr_round_w4(const void* src, int src_fmt, int64_t src_ld, size_t rows, size_t cols, uint8_t* codes, void* scales,
+                  int scale_fmt, int group, void* values, int64_t values_ld, int variant, int k_bits, uint64_t seed,
+                  uint64_t offset, void* cuda_stream);
+
 /* fbsr_round_bits -- the same rounding with caller-supplied random bits
  * (Section II-B treats the randomness as a finite string of bits handed to the
  * rounder).  rand_words: device, ceil(n / dpw) words; element i uses field

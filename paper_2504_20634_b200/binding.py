@@ -85,6 +85,11 @@ def _load():
     L.fbsr_qat_adamw_step.restype = i
     L.fbsr_adamw_multi.argtypes = [ctypes.POINTER(FbsrAdamwTensor), sz, i, i, i, i, i, u64, d, d, d, d, d, i, vp, vp]
     L.fbsr_adamw_multi.restype = i
+    i64 = ctypes.c_int64
+    L.fbsr_w4_padded.argtypes = [sz]
+    L.fbsr_w4_padded.restype = sz
+    L.fbsr_round_w4.argtypes = [vp, i, i64, sz, sz, vp, vp, i, i, vp, i64, i, i, u64, u64, vp]
+    L.fbsr_round_w4.restype = i
     L.fbsr_round_host_min_workspace.argtypes = []
     L.fbsr_round_host_min_workspace.restype = sz
     L.fbsr_round_host.argtypes = [vp, vp, sz, i, i, i, u64, u64, f, vp, sz, vp]
@@ -419,6 +424,55 @@ def fbsr_adamw_multi(tensors, variant, k_bits, seed, lr, beta1, beta2, eps, weig
                                    _var(variant), k_bits, seed, lr, beta1, beta2, eps, weight_decay, step, gs,
                                    _stream(tensors._w[0])), "fbsr_adamw_multi")
     return tensors
+
+
+W4_SCALE = {"e8m0": 0, "bf16": 1}                                 # FBSR_SCALE_*
+W4_SCALE_DTYPE = {"e8m0": torch.uint8, "bf16": torch.bfloat16}
+
+
+def _matrix(t, dtypes, what):
+    """(pointer, leading dimension) of a 2-D CUDA tensor whose rows are contiguous."""
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
+        raise TypeError("%s must be a 2-D CUDA tensor of %s" % (what, " or ".join(map(str, dtypes))))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise TypeError("%s must have contiguous rows" % what)
+    return ctypes.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def fbsr_w4_padded(cols):
+    """Columns of a 4-bit row with its padding: cols rounded up to a multiple of 128."""
+    return int(_L.fbsr_w4_padded(int(cols)))
+
+
+def fbsr_round_w4(src, variant, k_bits, seed, offset=0, group=32, scale_fmt="e8m0", values=None, out=None, scales=None):
+    """Round a matrix (float32, bfloat16 or float16; rows may be strided) to 4 bits with a scale per `group` elements of a
+    row; returns (codes uint8 [rows, padded / 2], scales [rows, padded / group]).  `values`, if given, receives the
+    values that the codes stand for (same shape and dtype as src, not overlapping it)."""
+    ps, ld = _matrix(src, tuple(SOURCE_TYPE), "src")
+    rows, cols = src.shape
+    padded = fbsr_w4_padded(cols)
+    if scale_fmt not in W4_SCALE:
+        raise ValueError("scale_fmt must be one of %s" % sorted(W4_SCALE))
+    sdt = W4_SCALE_DTYPE[scale_fmt]
+    if out is None:
+        out = torch.empty(rows, padded // 2, dtype=torch.uint8, device=src.device)
+    if scales is None:
+        scales = torch.empty(rows, padded // max(int(group), 1), dtype=sdt, device=src.device)
+    for t, shape, dt, what in ((out, (rows, padded // 2), torch.uint8, "out"),
+                               (scales, (rows, padded // max(int(group), 1)), sdt, "scales")):
+        if tuple(t.shape) != shape or t.device != src.device:
+            raise ValueError("%s must have shape %s on %s" % (what, shape, src.device))
+        _dev(t, dt, what)
+    pv, vld = None, 0
+    if values is not None:
+        if values.shape != src.shape or values.device != src.device:
+            raise ValueError("values must have the shape and device of src")
+        pv, vld = _matrix(values, (src.dtype,), "values")
+    with torch.cuda.device(src.device):
+        _check(_L.fbsr_round_w4(ps, SOURCE_TYPE[src.dtype], ld, rows, cols, ctypes.c_void_p(out.data_ptr()),
+                                ctypes.c_void_p(scales.data_ptr()), W4_SCALE[scale_fmt], int(group), pv, vld, _var(variant),
+                                k_bits, seed, offset, _stream(src)), "fbsr_round_w4")
+    return out, scales
 
 
 def fbsr_round_host(src_host, dst_host, fmt, variant, k_bits, seed, offset, scale, workspace):

@@ -18,9 +18,9 @@ LIB = os.path.join(HERE, "libfbsr.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-Xcompiler", "-O2", "--fmad=false"]
-HEADERS = ["fbsr_device.cuh", "fbsr_kernels.cuh", "fbsr_internal.h", os.path.join("..", "..", "include", "fbsr.h")]
+HEADERS = ["fbsr_device.cuh", "fbsr_kernels.cuh", "fbsr_w4.cuh", "fbsr_internal.h", os.path.join("..", "..", "include", "fbsr.h")]
 
-SINGLE_UNITS = ["fbsr_api", "fbsr_descriptor", "fbsr_adamw_multi"]      # sources compiled once, as they are
+SINGLE_UNITS = ["fbsr_api", "fbsr_descriptor", "fbsr_adamw_multi", "fbsr_round_w4"]      # sources compiled once, as they are
 
 
 def _units():
