@@ -90,6 +90,8 @@ def _load():
     L.fbsr_w4_padded.restype = sz
     L.fbsr_round_w4.argtypes = [vp, i, i64, sz, sz, vp, vp, i, i, vp, i64, i, i, u64, u64, vp]
     L.fbsr_round_w4.restype = i
+    L.fbsr_gemv_w4.argtypes = [vp, i, i64, sz, vp, vp, i, i, sz, sz, vp, i, i64, vp]
+    L.fbsr_gemv_w4.restype = i
     L.fbsr_round_host_min_workspace.argtypes = []
     L.fbsr_round_host_min_workspace.restype = sz
     L.fbsr_round_host.argtypes = [vp, vp, sz, i, i, i, u64, u64, f, vp, sz, vp]
@@ -473,6 +475,36 @@ def fbsr_round_w4(src, variant, k_bits, seed, offset=0, group=32, scale_fmt="e8m
                                 ctypes.c_void_p(scales.data_ptr()), W4_SCALE[scale_fmt], int(group), pv, vld, _var(variant),
                                 k_bits, seed, offset, _stream(src)), "fbsr_round_w4")
     return out, scales
+
+
+def fbsr_gemv_w4(x, codes, scales, group=32, out=None, out_dtype=None):
+    """x W^T for rows x [m, k] (bfloat16 or float16; rows may be strided) and a 4-bit matrix W [n, k] as fbsr_round_w4 returns
+    it.  The result [m, n] has out_dtype (float32, bfloat16 or float16; by default that of x).  A 1-D x gives a 1-D result."""
+    if x.dim() == 1:
+        if out is not None and out.dim() != 1:
+            raise ValueError("out must have one dimension as x has")
+        y = fbsr_gemv_w4(x[None], codes, scales, group, None if out is None else out[None], out_dtype)
+        return y[0] if out is None else out
+    px, ldx = _matrix(x, (torch.bfloat16, torch.float16), "x")
+    m, k = x.shape
+    group, padded = int(group), fbsr_w4_padded(k)
+    if codes.dim() != 2 or codes.shape[1] != padded // 2 or codes.device != x.device:
+        raise ValueError("codes must have shape (n, %d) on %s" % (padded // 2, x.device))
+    n = codes.shape[0]
+    if scales.dtype not in (torch.uint8, torch.bfloat16):
+        raise TypeError("scales must be uint8 or bfloat16")
+    if tuple(scales.shape) != (n, padded // max(group, 1)) or scales.device != x.device:
+        raise ValueError("scales must have shape (%d, %d) on %s" % (n, padded // max(group, 1), x.device))
+    if out is None:
+        out = torch.empty(m, n, dtype=out_dtype or x.dtype, device=x.device)
+    elif tuple(out.shape) != (m, n) or out.device != x.device or out_dtype not in (None, out.dtype):
+        raise ValueError("out must have shape (%d, %d) on %s and the dtype asked for" % (m, n, x.device))
+    py, ldy = _matrix(out, tuple(SOURCE_TYPE), "out")
+    with torch.cuda.device(x.device):
+        _check(_L.fbsr_gemv_w4(px, SOURCE_TYPE[x.dtype], ldx, m, _dev(codes, torch.uint8, "codes"),
+                               _dev(scales, scales.dtype, "scales"), 0 if scales.dtype == torch.uint8 else 1, group, n, k, py,
+                               SOURCE_TYPE[out.dtype], ldy, _stream(x)), "fbsr_gemv_w4")
+    return out
 
 
 def fbsr_round_host(src_host, dst_host, fmt, variant, k_bits, seed, offset, scale, workspace):

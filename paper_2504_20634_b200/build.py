@@ -20,7 +20,7 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std
          "-Xcompiler", "-fPIC", "-Xcompiler", "-O2", "--fmad=false"]
 HEADERS = ["fbsr_device.cuh", "fbsr_kernels.cuh", "fbsr_w4.cuh", "fbsr_internal.h", os.path.join("..", "..", "include", "fbsr.h")]
 
-SINGLE_UNITS = ["fbsr_api", "fbsr_descriptor", "fbsr_adamw_multi", "fbsr_round_w4"]      # sources compiled once, as they are
+SINGLE_UNITS = ["fbsr_api", "fbsr_descriptor", "fbsr_adamw_multi", "fbsr_round_w4", "fbsr_gemv_w4"]      # sources compiled once, as they are
 
 
 def _units():
