@@ -21,7 +21,8 @@ _BINDING_NAMES = (
 def __getattr__(name):
     # Loaded on first use so that the build module can be imported before the library exists.
     if name in _BINDING_NAMES:
-        return getattr(importlib.import_module(".binding", __name__), name)
+        value = globals()[name] = getattr(importlib.import_module(".binding", __name__), name)      # found directly from now on
+        return value
     raise AttributeError("module %r has no attribute %r" % (__name__, name))
 
 

@@ -5,6 +5,7 @@ Argument marshalling only.  Tensors must live on a CUDA device (except for
 output tensors are allocated with torch when not supplied.  Calls are enqueued on
 torch's current stream of the tensors' device.
 """
+import contextlib
 import ctypes
 import os
 
@@ -421,10 +422,12 @@ def fbsr_adamw_multi(tensors, variant, k_bits, seed, lr, beta1, beta2, eps, weig
         if grad_scale.numel() != 1 or grad_scale.device != tensors.device:
             raise ValueError("grad_scale must be one element on %s" % tensors.device)
         gs = _dev(grad_scale, torch.float32, "grad_scale")
-    with torch.cuda.device(tensors.device):
-        _check(_L.fbsr_adamw_multi(tensors.array, tensors.count, tensors.state_bits, tensors.g_fmt, _fmt(tensors.fmt),
-                                   _var(variant), k_bits, seed, lr, beta1, beta2, eps, weight_decay, step, gs,
-                                   _stream(tensors._w[0])), "fbsr_adamw_multi")
+    device = tensors.device.index
+    with _on(device):
+        status = _L.fbsr_adamw_multi(tensors.array, tensors.count, tensors.state_bits, tensors.g_fmt, _fmt(tensors.fmt),
+                                     _var(variant), k_bits, seed, lr, beta1, beta2, eps, weight_decay, step, gs, _raw_stream(device))
+    if status:
+        _check(status, "fbsr_adamw_multi")
     return tensors
 
 
@@ -432,13 +435,26 @@ W4_SCALE = {"e8m0": 0, "bf16": 1}                                 # FBSR_SCALE_*
 W4_SCALE_DTYPE = {"e8m0": torch.uint8, "bf16": torch.bfloat16}
 
 
+_SOURCES = (torch.float32, torch.bfloat16, torch.float16)
+_HALF = (torch.bfloat16, torch.float16)
+_HERE_ALREADY = contextlib.nullcontext()
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _on(device):
+    """A context with CUDA device `device` (an ordinal) current: nothing to do, and nothing spent, where it is already."""
+    return _HERE_ALREADY if torch._C._cuda_getDevice() == device else torch.cuda.device(device)
+
+
 def _matrix(t, dtypes, what):
-    """(pointer, leading dimension) of a 2-D CUDA tensor whose rows are contiguous."""
-    if not (t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
+    """(address, leading dimension) of a 2-D CUDA tensor whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
         raise TypeError("%s must be a 2-D CUDA tensor of %s" % (what, " or ".join(map(str, dtypes))))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise TypeError("%s must have contiguous rows" % what)
-    return ctypes.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), (ld if rows > 1 and ld > cols else cols)
 
 
 def fbsr_w4_padded(cols):
@@ -450,30 +466,30 @@ def fbsr_round_w4(src, variant, k_bits, seed, offset=0, group=32, scale_fmt="e8m
     """Round a matrix (float32, bfloat16 or float16; rows may be strided) to 4 bits with a scale per `group` elements of a
     row; returns (codes uint8 [rows, padded / 2], scales [rows, padded / group]).  `values`, if given, receives the
     values that the codes stand for (same shape and dtype as src, not overlapping it)."""
-    ps, ld = _matrix(src, tuple(SOURCE_TYPE), "src")
+    ps, ld = _matrix(src, _SOURCES, "src")
     rows, cols = src.shape
-    padded = fbsr_w4_padded(cols)
+    device, group, half_row = src.get_device(), int(group), (cols + 127) // 128 * 64
     if scale_fmt not in W4_SCALE:
         raise ValueError("scale_fmt must be one of %s" % sorted(W4_SCALE))
-    sdt = W4_SCALE_DTYPE[scale_fmt]
+    scale_dtype, groups = W4_SCALE_DTYPE[scale_fmt], 2 * half_row // max(group, 1)
     if out is None:
-        out = torch.empty(rows, padded // 2, dtype=torch.uint8, device=src.device)
+        out = src.new_empty((rows, half_row), dtype=torch.uint8)
+    elif out.dtype is not torch.uint8 or out.shape != (rows, half_row) or out.get_device() != device or not out.is_contiguous():
+        raise ValueError("out must be a contiguous uint8 tensor of shape (%d, %d) on %s" % (rows, half_row, src.device))
     if scales is None:
-        scales = torch.empty(rows, padded // max(int(group), 1), dtype=sdt, device=src.device)
-    for t, shape, dt, what in ((out, (rows, padded // 2), torch.uint8, "out"),
-                               (scales, (rows, padded // max(int(group), 1)), sdt, "scales")):
-        if tuple(t.shape) != shape or t.device != src.device:
-            raise ValueError("%s must have shape %s on %s" % (what, shape, src.device))
-        _dev(t, dt, what)
+        scales = src.new_empty((rows, groups), dtype=scale_dtype)
+    elif scales.dtype is not scale_dtype or scales.shape != (rows, groups) or scales.get_device() != device or not scales.is_contiguous():
+        raise ValueError("scales must be a contiguous %s tensor of shape (%d, %d) on %s" % (scale_dtype, rows, groups, src.device))
     pv, vld = None, 0
     if values is not None:
-        if values.shape != src.shape or values.device != src.device:
+        if values.shape != src.shape or values.get_device() != device:
             raise ValueError("values must have the shape and device of src")
         pv, vld = _matrix(values, (src.dtype,), "values")
-    with torch.cuda.device(src.device):
-        _check(_L.fbsr_round_w4(ps, SOURCE_TYPE[src.dtype], ld, rows, cols, ctypes.c_void_p(out.data_ptr()),
-                                ctypes.c_void_p(scales.data_ptr()), W4_SCALE[scale_fmt], int(group), pv, vld, _var(variant),
-                                k_bits, seed, offset, _stream(src)), "fbsr_round_w4")
+    with _on(device):
+        status = _L.fbsr_round_w4(ps, SOURCE_TYPE[src.dtype], ld, rows, cols, out.data_ptr(), scales.data_ptr(), W4_SCALE[scale_fmt],
+                                  group, pv, vld, _var(variant), k_bits, seed, offset, _raw_stream(device))
+    if status:
+        _check(status, "fbsr_round_w4")
     return out, scales
 
 
@@ -485,25 +501,27 @@ def fbsr_gemv_w4(x, codes, scales, group=32, out=None, out_dtype=None):
             raise ValueError("out must have one dimension as x has")
         y = fbsr_gemv_w4(x[None], codes, scales, group, None if out is None else out[None], out_dtype)
         return y[0] if out is None else out
-    px, ldx = _matrix(x, (torch.bfloat16, torch.float16), "x")
+    px, ldx = _matrix(x, _HALF, "x")
     m, k = x.shape
-    group, padded = int(group), fbsr_w4_padded(k)
-    if codes.dim() != 2 or codes.shape[1] != padded // 2 or codes.device != x.device:
-        raise ValueError("codes must have shape (n, %d) on %s" % (padded // 2, x.device))
+    device, group, half_row = x.get_device(), int(group), (k + 127) // 128 * 64
     n = codes.shape[0]
-    if scales.dtype not in (torch.uint8, torch.bfloat16):
+    if codes.dtype is not torch.uint8 or codes.shape != (n, half_row) or codes.get_device() != device or not codes.is_contiguous():
+        raise ValueError("codes must be a contiguous uint8 tensor of shape (n, %d) on %s" % (half_row, x.device))
+    scale_fmt = 0 if scales.dtype is torch.uint8 else 1
+    if scale_fmt and scales.dtype is not torch.bfloat16:
         raise TypeError("scales must be uint8 or bfloat16")
-    if tuple(scales.shape) != (n, padded // max(group, 1)) or scales.device != x.device:
-        raise ValueError("scales must have shape (%d, %d) on %s" % (n, padded // max(group, 1), x.device))
+    if scales.shape != (n, 2 * half_row // max(group, 1)) or scales.get_device() != device or not scales.is_contiguous():
+        raise ValueError("scales must be a contiguous tensor of shape (%d, %d) on %s" % (n, 2 * half_row // max(group, 1), x.device))
     if out is None:
-        out = torch.empty(m, n, dtype=out_dtype or x.dtype, device=x.device)
-    elif tuple(out.shape) != (m, n) or out.device != x.device or out_dtype not in (None, out.dtype):
+        out = x.new_empty((m, n), dtype=out_dtype)
+    elif out.shape != (m, n) or out.get_device() != device or out_dtype not in (None, out.dtype):
         raise ValueError("out must have shape (%d, %d) on %s and the dtype asked for" % (m, n, x.device))
-    py, ldy = _matrix(out, tuple(SOURCE_TYPE), "out")
-    with torch.cuda.device(x.device):
-        _check(_L.fbsr_gemv_w4(px, SOURCE_TYPE[x.dtype], ldx, m, _dev(codes, torch.uint8, "codes"),
-                               _dev(scales, scales.dtype, "scales"), 0 if scales.dtype == torch.uint8 else 1, group, n, k, py,
-                               SOURCE_TYPE[out.dtype], ldy, _stream(x)), "fbsr_gemv_w4")
+    py, ldy = _matrix(out, _SOURCES, "out")
+    with _on(device):
+        status = _L.fbsr_gemv_w4(px, SOURCE_TYPE[x.dtype], ldx, m, codes.data_ptr(), scales.data_ptr(), scale_fmt, group, n, k, py,
+                                 SOURCE_TYPE[out.dtype], ldy, _raw_stream(device))
+    if status:
+        _check(status, "fbsr_gemv_w4")
     return out
 
 

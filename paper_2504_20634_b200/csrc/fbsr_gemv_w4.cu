@@ -9,19 +9,25 @@
 // stay exact, scales are applied in binary32.  (The fifth-generation unit would take 128-row tiles from shared memory:
 // the decoded weights would have to be written there and read back, for a product that is far from compute-bound.)
 //
-// A CTA takes 16 RT rows of W; its eight warps share out the row's blocks of 128 columns and add their sums in shared
-// memory in a fixed order.  Row g of a 16-row tile is read by four lanes, 16 bytes each, and lane t's words of the four
-// quarters of the block meet x's elements [32 j + 8 t, + 8): the order of k inside the matrix instruction is the same
-// permutation on both sides.
+// A CTA takes 128 rows of W, 16 to a warp, and a range of the columns; up to eight CTAs of a cluster share the columns of
+// the same rows and add their sums over distributed shared memory in a fixed order.  Many rows against a short range of
+// columns keep the work on x small: it is staged once per CTA, m values a column against 128 codes.  Row g of a warp's tile
+// is read by four lanes, 16 bytes each, and lane t's words of the four quarters of a block of 128 columns meet x's elements
+// [32 j + 8 t, + 8): the order of k inside the matrix instruction is the same permutation on both sides.  Four blocks are in
+// flight per warp.
 //
 // x is staged in shared memory in binary16.  bfloat16 rows are first multiplied by the power of two that brings the row's
 // largest finite magnitude to [2^14, 2^15): elements down to 2^-32 of it keep all their 8 bits, smaller ones are rounded
 // to 2^-40 of it, far below the rounding of the binary32 sums; the sum is multiplied back at the end.
-#include <cmath>
+#include <atomic>
+
+#include <cooperative_groups.h>
 
 #include "../../include/fbsr.h"
 #include "fbsr_internal.h"
 #include "fbsr_w4.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace fbsr {
 namespace {
@@ -29,8 +35,9 @@ namespace {
 constexpr int GEMV_WARPS = 8;
 constexpr int GEMV_THREADS = GEMV_WARPS * 32;
 constexpr int GEMV_MAX_M = 32;                   // rows of x a launch takes
-constexpr int X_SMEM = 72 * 1024;                // shared memory for a chunk of x
-constexpr int CHUNK_GRAIN = W4_BLOCK * GEMV_WARPS;
+constexpr int RUN = 4;                           // blocks of 128 columns of a stage
+constexpr int TILE = 16;                         // rows of W a warp takes
+constexpr int ROW_PITCH = RUN * W4_BLOCK_BYTES;  // of a row of codes in shared memory
 
 struct GemvArgs {
     const uint16_t* x;
@@ -39,39 +46,51 @@ struct GemvArgs {
     void* y;
     int64_t ldx, ldy;
     uint32_t n, k, blocks;                       // blocks: of 128 columns, one row of W
-    uint32_t row_scale_bytes, block_scale_bytes; // bytes of scales of a row / of a block of 128
-    int m, chunk, out_fmt, scale_bf16;
+    uint32_t row_scale_bytes;
+    int m, chunk_runs, out_fmt, warps_k;
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The scales of one block of one row as stored: one, two, four or eight bytes.
-__device__ __forceinline__ uint2 load_scales(const uint8_t* p, uint32_t bytes)
+// The same into sums that start from zero.
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    uint2 r = make_uint2(0u, 0u);
-    if (bytes == 4) r.x = __ldg(reinterpret_cast<const uint32_t*>(p));
-    else if (bytes == 8) r = __ldg(reinterpret_cast<const uint2*>(p));
-    else if (bytes == 2) r.x = __ldg(reinterpret_cast<const uint16_t*>(p));
-    else r.x = __ldg(p);
-    return r;
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// The scale of quarter j (32 elements) of the block.
-__device__ __forceinline__ float quarter_scale(const uint2& raw, int j, const GemvArgs& a)
+// The COUNT scales of a block (SB bytes at p, in shared memory) as numbers.
+template <bool BF16_S, int COUNT>
+__device__ __forceinline__ void block_scales(const unsigned char* p, float (&s)[COUNT])
 {
-    if (a.scale_bf16) {
-        // 8, 4 or 2 bytes: four, two or one scales
-        const int i = a.block_scale_bytes == 8 ? j : a.block_scale_bytes == 4 ? j >> 1 : 0;
-        const uint32_t w = i >= 2 ? raw.y : raw.x;
-        return __uint_as_float((i & 1) ? (w & 0xFFFF0000u) : (w << 16));
+    constexpr int SB = COUNT * (BF16_S ? 2 : 1);
+    uint32_t w[SB == 8 ? 2 : 1];
+    if constexpr (SB == 8) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else if constexpr (SB == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+    else if constexpr (SB == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
+    else w[0] = *p;
+#pragma unroll
+    for (int i = 0; i < COUNT; i += 2) {         // scales i and i + 1 as bfloat16
+        const uint32_t pair = BF16_S ? w[i / 2] : e8m0_pair_to_bf16x2(i ? w[0] >> 16 : w[0]);
+        s[i] = __uint_as_float(pair << 16);
+        if constexpr (COUNT > 1) s[i + 1] = __uint_as_float(pair & 0xFFFF0000u);
     }
-    const int i = a.block_scale_bytes == 4 ? j : a.block_scale_bytes == 2 ? j >> 1 : 0;
-    return e8m0_value((raw.x >> (8 * i)) & 0xFFu);
+}
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(unsigned char* smem_dst, const uint8_t* gmem_src)
+{
+    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem_dst);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(gmem_src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(gmem_src) : "memory");
 }
 
 // Eight elements of a row of x from column k on, zero beyond the row's end.
@@ -86,179 +105,326 @@ __device__ __forceinline__ uint4 load_x8(const GemvArgs& a, int row, uint32_t k)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Power of two that brings a row whose largest finite magnitude has the bfloat16 pattern `top` to [2^14, 2^15).
-__device__ __forceinline__ float row_factor(uint32_t top)
+__device__ __forceinline__ void store_y(const GemvArgs& a, int col, uint32_t row, float sum)
 {
-    const int e = (int)(top >> 7) - 127;                           // subnormal or zero: -127
-    return __uint_as_float((uint32_t)(min(14 - e, 127) + 127) << 23);
+    if (col >= a.m || row >= a.n) return;
+    const int64_t at = (int64_t)col * a.ldy + row;
+    if (a.out_fmt == FBSR_FP32) static_cast<float*>(a.y)[at] = sum;
+    else if (a.out_fmt == FBSR_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(sum);
+    else static_cast<__half*>(a.y)[at] = __float2half_rn(sum);
 }
 
-template <bool BF16_X, int NT, int RT>
-__global__ void __launch_bounds__(GEMV_THREADS)
-gemv_w4_kernel(const __grid_constant__ GemvArgs a)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ uint32_t row_top[GEMV_MAX_M];
-    __half* xs = reinterpret_cast<__half*>(smem);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const uint32_t row0 = blockIdx.x * (16 * RT);
-    const int stride = a.chunk + 32;             // elements: 64 bytes more, so that two rows' quarters meet different banks
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
 
-    if constexpr (BF16_X) {
-        if (threadIdx.x < GEMV_MAX_M) row_top[threadIdx.x] = 0u;
-        __syncthreads();
-        const uint32_t units = a.blocks * (W4_BLOCK / 8);
-        for (int row = 0; row < a.m; ++row) {
-            uint32_t top = 0u;
-            for (uint32_t u = threadIdx.x; u < units; u += GEMV_THREADS) {
-                const uint4 v = load_x8(a, row, u * 8);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Largest finite magnitude pattern among eight bfloat16 numbers.
+__device__ __forceinline__ uint32_t top_of8(const uint4& v)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t top = 0u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint32_t lo = w[c] & 0x7FFFu, hi = (w[c] >> 16) & 0x7FFFu;
+        top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+    }
+    return top;
+}
+
+// `blocks` blocks of 128 columns of x, from block `first` on, to shared memory as binary16; COLS: rows of x provided for.
+// Sixteen lanes hold a block of a row, eight elements each; up to four such loads are in flight per thread.
+template <bool BF16_X, int COLS>
+__device__ __forceinline__ void stage_x(const GemvArgs& a, uint32_t first, uint32_t blocks, __half* xs, int stride, float* factor)
+{
+    constexpr int FLIGHT = 4, LANES = W4_BLOCK / 8, GROUPS = GEMV_THREADS / LANES;
+    const uint32_t lane = threadIdx.x % LANES, total = blocks * (COLS == 1 ? 1u : (uint32_t)a.m);
+    // group i of sixteen threads takes blocks i, i + GROUPS, ... of all rows' blocks
+    uint32_t row = 0, block = threadIdx.x / LANES;
+    for (uint32_t done = 0; done < total; done += FLIGHT * GROUPS) {
+        uint4 v[FLIGHT];
+        uint32_t r[FLIGHT], b[FLIGHT];
+#pragma unroll
+        for (int i = 0; i < FLIGHT; ++i) {
+            while (COLS > 1 && block >= blocks && row < (uint32_t)a.m) { block -= blocks; ++row; }
+            r[i] = row; b[i] = block;
+            const bool inside = COLS > 1 ? row < (uint32_t)a.m : block < blocks;
+            if (!inside) r[i] = 0xFFFFFFFFu;
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (inside) v[i] = load_x8(a, row, (first + block) * W4_BLOCK + lane * 8);
+            block += GROUPS;
+        }
+#pragma unroll
+        for (int i = 0; i < FLIGHT; ++i) {
+            if (done + i * GROUPS >= total) break;           // the same for all threads
+            if constexpr (BF16_X) {
+                uint32_t top = top_of8(v[i]);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+                // 2^(14 - e), e the exponent of the largest, as far as binary32 has it; and its inverse
+                const int f = min(14 - ((int)(top >> 7) - 127), 126);
+                const float up = __uint_as_float((uint32_t)(127 + f) << 23), down = __uint_as_float((uint32_t)(127 - f) << 23);
+                uint32_t* w = reinterpret_cast<uint32_t*>(&v[i]);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const uint32_t lo = w[c] & 0x7FFFu, hi = (w[c] >> 16) & 0x7FFFu;
-                    top = max(top, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+                    const __half2 h = __floats2half2_rn(__fmul_rn(__uint_as_float(w[c] << 16), up),
+                                                        __fmul_rn(__uint_as_float(w[c] & 0xFFFF0000u), up));
+                    w[c] = *reinterpret_cast<const uint32_t*>(&h);
                 }
+                if (r[i] != 0xFFFFFFFFu && lane == 0) factor[b[i] * COLS + r[i]] = down;
             }
-            top = __reduce_max_sync(0xFFFFFFFFu, top);
-            if (lane == 0) atomicMax(&row_top[row], top);
+            if (r[i] != 0xFFFFFFFFu) *reinterpret_cast<uint4*>(xs + (size_t)r[i] * stride + b[i] * W4_BLOCK + lane * 8) = v[i];
         }
-    }
-
-    float acc[RT][NT][4];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[r][n][i] = 0.0f;
-
-    // this lane's two rows of each tile; rows beyond the matrix read its last row and are dropped at the end
-    const uint8_t* code_row[RT][2];
-    const uint8_t* scale_row[RT][2];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t row = min(row0 + 16 * r + 8 * h + g, a.n - 1);
-            code_row[r][h] = a.codes + (uint64_t)row * a.blocks * W4_BLOCK_BYTES + t * 16;
-            scale_row[r][h] = a.scales + (uint64_t)row * a.row_scale_bytes;
-        }
-
-    const uint32_t padded = a.blocks * W4_BLOCK;
-    for (uint32_t k0 = 0; k0 < padded; k0 += a.chunk) {
-        const uint32_t len = min((uint32_t)a.chunk, padded - k0);
-        __syncthreads();                         // the previous chunk has been read (first: the rows' maxima are complete)
-        for (int row = 0; row < a.m; ++row) {
-            float factor = 1.0f;
-            if constexpr (BF16_X) factor = row_factor(row_top[row]);
-            for (uint32_t u = threadIdx.x; u < len / 8; u += GEMV_THREADS) {
-                uint4 v = load_x8(a, row, k0 + u * 8);
-                if constexpr (BF16_X) {
-                    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const __half2 h = __floats2half2_rn(__fmul_rn(__uint_as_float(w[c] << 16), factor),
-                                                            __fmul_rn(__uint_as_float(w[c] & 0xFFFF0000u), factor));
-                        w[c] = *reinterpret_cast<const uint32_t*>(&h);
-                    }
-                }
-                *reinterpret_cast<uint4*>(xs + (size_t)row * stride + u * 8) = v;
-            }
-        }
-        __syncthreads();
-        for (uint32_t s = warp; s < len / W4_BLOCK; s += GEMV_WARPS) {
-            const uint32_t block = k0 / W4_BLOCK + s;
-            uint4 b[NT][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    b[n][j] = make_uint4(0u, 0u, 0u, 0u);
-                    if (8 * n + g < a.m)
-                        b[n][j] = *reinterpret_cast<const uint4*>(xs + (size_t)(8 * n + g) * stride + s * W4_BLOCK + 32 * j + 8 * t);
-                }
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const uint4 lo = __ldg(reinterpret_cast<const uint4*>(code_row[r][0] + (uint64_t)block * W4_BLOCK_BYTES));
-                const uint4 hi = __ldg(reinterpret_cast<const uint4*>(code_row[r][1] + (uint64_t)block * W4_BLOCK_BYTES));
-                const uint2 s_lo = load_scales(scale_row[r][0] + (uint64_t)block * a.block_scale_bytes, a.block_scale_bytes);
-                const uint2 s_hi = load_scales(scale_row[r][1] + (uint64_t)block * a.block_scale_bytes, a.block_scale_bytes);
-                const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t pl[4], ph[4];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        pl[p] = e2m1_pair_to_half2(wl[j] >> (8 * p));
-                        ph[p] = e2m1_pair_to_half2(wh[j] >> (8 * p));
-                    }
-                    const float sl = quarter_scale(s_lo, j, a), sh = quarter_scale(s_hi, j, a);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        mma_f16(part, pl[0], ph[0], pl[1], ph[1], b[n][j].x, b[n][j].y);
-                        mma_f16(part, pl[2], ph[2], pl[3], ph[3], b[n][j].z, b[n][j].w);
-                        acc[r][n][0] = __fmaf_rn(sl, part[0], acc[r][n][0]);
-                        acc[r][n][1] = __fmaf_rn(sl, part[1], acc[r][n][1]);
-                        acc[r][n][2] = __fmaf_rn(sh, part[2], acc[r][n][2]);
-                        acc[r][n][3] = __fmaf_rn(sh, part[3], acc[r][n][3]);
-                    }
-                }
-            }
-        }
-    }
-
-    // the warps' sums, [warp][x row][W row], over the staged x
-    __syncthreads();
-    float* red = reinterpret_cast<float*>(smem);
-    constexpr int ROWS = 16 * RT, TILE = ROWS * 8 * NT;
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                red[warp * TILE + (8 * n + 2 * t + (i & 1)) * ROWS + 16 * r + g + 8 * (i >> 1)] = acc[r][n][i];
-    __syncthreads();
-    for (int i = threadIdx.x; i < TILE; i += GEMV_THREADS) {
-        const int col = i / ROWS;
-        const uint32_t row = row0 + i % ROWS;
-        if (col >= a.m || row >= a.n) continue;
-        float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < GEMV_WARPS; ++w) sum = __fadd_rn(sum, red[w * TILE + i]);
-        if constexpr (BF16_X) sum = __fdiv_rn(sum, row_factor(row_top[col]));        // a power of two
-        const int64_t at = (int64_t)col * a.ldy + row;
-        if (a.out_fmt == FBSR_FP32) static_cast<float*>(a.y)[at] = sum;
-        else if (a.out_fmt == FBSR_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(sum);
-        else static_cast<__half*>(a.y)[at] = __float2half_rn(sum);
     }
 }
 
-template <bool BF16_X, int NT, int RT>
+// BF16_X: x holds bfloat16.  BF16_S, COUNT: scales are bfloat16, COUNT of them in a block of 128.  ONE: x is one row, which
+// column 0 of the sums stands for alone.  NT: groups of 8 rows of x.  STAGES: of each warp's ring.
+template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int NT, int STAGES>
+__global__ void __launch_bounds__(GEMV_THREADS, 2)
+gemv_w4_kernel(const __grid_constant__ GemvArgs a)
+{
+    constexpr int SB = COUNT * (BF16_S ? 2 : 1); // bytes of scales of a block
+    constexpr int COLS = ONE ? 1 : 8 * NT;
+    constexpr int QUARTERS = 4 / COUNT;          // quarters of a block under one scale
+    constexpr int STEP = ONE ? 2 : 1;            // of the four sums of a lane, those of column 0 are the first and the third
+    constexpr int STAGE = TILE * (ROW_PITCH + RUN * SB);
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), g = lane >> 2, t = lane & 3;
+    const int rows = GEMV_WARPS * TILE / a.warps_k, warp_row = warp / a.warps_k, warp_k = warp % a.warps_k;
+    const uint32_t row0 = blockIdx.x * rows + warp_row * TILE;
+    const int stride = a.chunk_runs * (RUN * W4_BLOCK) + 32;       // elements: 64 bytes more, so that two rows meet different banks
+    unsigned char* ring = smem + warp * (STAGES * STAGE);
+    float* red = reinterpret_cast<float*>(smem);                   // at the end, over the rings: [warps_k][m][rows]
+    float* factor = reinterpret_cast<float*>(smem + GEMV_WARPS * STAGES * STAGE);      // BF16_X: [block of the chunk][COLS]
+    __half* xs = reinterpret_cast<__half*>(factor + (BF16_X ? (a.chunk_runs * RUN * COLS + 3) / 4 * 4 : 0));
+
+    // this CTA's runs of blocks; warp_k of them is this warp's first, and every warps_k-th after it
+    const uint32_t runs = (a.blocks + RUN - 1) / RUN;
+    const uint32_t q_begin = (uint32_t)((uint64_t)runs * blockIdx.y / gridDim.y), q_end = (uint32_t)((uint64_t)runs * (blockIdx.y + 1) / gridDim.y);
+
+    // Each warp fills its own ring, sixteen lanes to a row of 256 bytes; odd rows have neighbouring 64 bytes exchanged so that
+    // the lanes that read two rows together meet different banks.  The rows' scales follow as words.  Rows beyond the matrix
+    // are left as they are: what comes of them is dropped.
+    const uint32_t tile_rows = row0 >= a.n ? 0u : min((uint32_t)TILE, a.n - row0), pitch = a.blocks * W4_BLOCK_BYTES;
+    const uint8_t* copy_src = a.codes + (uint64_t)(row0 + (lane >> 4)) * pitch + (lane & 15) * 16;
+    const uint32_t copy_dst = (lane >> 4) * ROW_PITCH + ((lane & 15) ^ ((lane >> 4) << 2)) * 16;
+    const bool scales_by_4 = a.row_scale_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0;
+    auto issue = [&](uint32_t q, int slot) {
+        if (q < q_end) {
+            unsigned char* to = ring + slot * STAGE;
+            const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
+            if ((uint32_t)(lane & 15) < here * 4) {
+#pragma unroll
+                for (int r = 0; r < TILE; r += 2)
+                    if (r + (lane >> 4) < tile_rows) copy_async<16>(to + copy_dst + r * ROW_PITCH, copy_src + (uint64_t)r * pitch + q * ROW_PITCH);
+            }
+            constexpr int WORDS = RUN * SB / 4;                    // of a row's scales of this stage
+            unsigned char* scales_to = to + TILE * ROW_PITCH;
+            const uint8_t* from = a.scales + q * (RUN * SB);
+            if (scales_by_4) {
+#pragma unroll
+                for (int i = 0; i < (TILE * WORDS + 31) / 32; ++i) {
+                    const uint32_t item = i * 32 + lane, row = item / WORDS, word = item % WORDS;
+                    if (row < tile_rows && word * 4 < here * SB)
+                        copy_async<4>(scales_to + item * 4, from + (uint64_t)(row0 + row) * a.row_scale_bytes + word * 4);
+                }
+            } else if (lane < tile_rows) {                         // rows of scales off the word grid: byte by byte
+                for (uint32_t i = 0; i < here * SB; ++i)
+                    scales_to[lane * (RUN * SB) + i] = __ldg(from + (uint64_t)(row0 + lane) * a.row_scale_bytes + i);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // the first stages are on their way before x is staged
+    const uint32_t q_first = q_begin + warp_k;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) issue(q_first + s * a.warps_k, s);
+
+    float acc[NT][4];
+    const __half* x_lane[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+        // columns beyond row m are computed and dropped
+        x_lane[n] = xs + (size_t)(ONE ? 0 : min(8 * n + g, a.m - 1)) * stride + 8 * t;
+    }
+
+    int slot = 0, next_slot = STAGES - 1;
+    for (uint32_t q0 = q_begin; q0 < q_end; q0 += a.chunk_runs) {
+        const uint32_t q1 = min(q0 + (uint32_t)a.chunk_runs, q_end);
+        if (q0 > q_begin) __syncthreads();       // the previous chunk has been read
+        stage_x<BF16_X, COLS>(a, q0 * RUN, (q1 - q0) * RUN, xs, stride, factor);
+        __syncthreads();
+        for (uint32_t q = q0 + warp_k; q < q1; q += a.warps_k) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+            __syncwarp();                        // this stage has arrived for all lanes, and all have read the one before it
+            issue(q + (STAGES - 1) * a.warps_k, next_slot);
+            const unsigned char* from = ring + slot * STAGE;
+            const unsigned char* codes_of[2] = {from + g * ROW_PITCH + (g & 1) * 64 + t * 16, from + g * ROW_PITCH + ((g & 1) ^ 1) * 64 + t * 16};
+            const unsigned char* scales_of = from + TILE * ROW_PITCH + g * (RUN * SB);
+            const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
+#pragma unroll
+            for (int d = 0; d < RUN; ++d) {
+                if (d >= here) break;
+                const uint32_t x_block = (q - q0) * RUN + d;
+                uint4 code[2];
+                float s[2][COUNT], sum[NT][4];               // scales and sums of the block
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    code[h] = *reinterpret_cast<const uint4*>(codes_of[d & 1] + 8 * h * ROW_PITCH + (d & ~1) * W4_BLOCK_BYTES);
+                    block_scales<BF16_S, COUNT>(scales_of + 8 * h * (RUN * SB) + d * SB, s[h]);
+                }
+#pragma unroll
+                for (int i = 0; i < COUNT; ++i) {
+                    float part[NT][4];                       // of the codes under one scale
+#pragma unroll
+                    for (int qu = 0; qu < QUARTERS; ++qu) {
+                        const int j = i * QUARTERS + qu;
+                        uint32_t lo[4], hi[4];
+                        e2m1_word_to_half2(word_of(code[0], j), lo);
+                        e2m1_word_to_half2(word_of(code[1], j), hi);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint4 b = *reinterpret_cast<const uint4*>(x_lane[n] + x_block * W4_BLOCK + 32 * j);
+                            if (qu == 0) mma_f16_first(part[n], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
+                            else mma_f16(part[n], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
+                            mma_f16(part[n], lo[2], hi[2], lo[3], hi[3], b.z, b.w);
+                        }
+                    }
+                    float (&into)[NT][4] = BF16_X ? sum : acc;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < 4; c += STEP) {
+                            const float sc = s[c >> 1][i];
+                            into[n][c] = BF16_X && i == 0 ? __fmul_rn(sc, part[n][c]) : __fmaf_rn(sc, part[n][c], into[n][c]);
+                        }
+                }
+                if constexpr (BF16_X) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float f[2];
+                        if constexpr (ONE) f[0] = factor[x_block];
+                        else {
+                            const float2 both = *reinterpret_cast<const float2*>(factor + x_block * COLS + 8 * n + 2 * t);
+                            f[0] = both.x; f[1] = both.y;
+                        }
+#pragma unroll
+                        for (int c = 0; c < 4; c += STEP) acc[n][c] = __fmaf_rn(f[c & 1], sum[n][c], acc[n][c]);
+                    }
+                }
+            }
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            next_slot = next_slot + 1 == STAGES ? 0 : next_slot + 1;
+        }
+    }
+    const bool alone = gridDim.y == 1 && a.warps_k == 1;
+    if (!alone) __syncthreads();                 // the rings have been read
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = 8 * n + 2 * t + (i & 1), row = warp_row * TILE + g + 8 * (i >> 1);
+            if (col >= a.m) continue;
+            if (alone) store_y(a, col, blockIdx.x * rows + row, acc[n][i]);
+            else red[(warp_k * a.m + col) * rows + row] = acc[n][i];
+        }
+    if (alone) return;
+    if (gridDim.y == 1) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * a.m; i += GEMV_THREADS) {
+            float total = 0.0f;
+            for (int w = 0; w < a.warps_k; ++w) total = __fadd_rn(total, red[w * a.m * rows + i]);
+            store_y(a, i / rows, blockIdx.x * rows + i % rows, total);
+        }
+        return;
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    // each CTA of the cluster adds up its share of the sums
+    for (uint32_t i = blockIdx.y * GEMV_THREADS + threadIdx.x; i < (uint32_t)(rows * a.m); i += gridDim.y * GEMV_THREADS) {
+        float total = 0.0f;
+        for (uint32_t c = 0; c < gridDim.y; ++c) {
+            const float* theirs = cluster.map_shared_rank(red, c);
+            for (int w = 0; w < a.warps_k; ++w) total = __fadd_rn(total, theirs[w * a.m * rows + i]);
+        }
+        store_y(a, i / rows, blockIdx.x * rows + i % rows, total);
+    }
+    cluster.sync();                              // nobody leaves while others read its sums
+}
+
+template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int NT, int STAGES>
 int launch(GemvArgs a, cudaStream_t stream)
 {
-    auto kernel = gemv_w4_kernel<BF16_X, NT, RT>;
-    const int padded = (int)(a.blocks * W4_BLOCK);
-    a.chunk = (X_SMEM / (2 * a.m) - 32) / CHUNK_GRAIN * CHUNK_GRAIN;
-    if (a.chunk > padded) a.chunk = padded;
-    const int x_bytes = a.m * (a.chunk + 32) * 2, red_bytes = GEMV_WARPS * 16 * RT * 8 * NT * 4;
-    const int bytes = x_bytes > red_bytes ? x_bytes : red_bytes;
-    if (bytes > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
-        return FBSR_ERR_CUDA;
-    const unsigned grid = (a.n + 16 * RT - 1) / (16 * RT);
-    kernel<<<grid, GEMV_THREADS, bytes, stream>>>(a);
+    auto kernel = gemv_w4_kernel<BF16_X, BF16_S, COUNT, ONE, NT, STAGES>;
+    constexpr int COLS = ONE ? 1 : 8 * NT, STAGE = TILE * (ROW_PITCH + RUN * COUNT * (BF16_S ? 2 : 1));
+    constexpr int RINGS = GEMV_WARPS * STAGES * STAGE, RUN_COLUMNS = RUN * W4_BLOCK;
+    static_assert(GEMV_WARPS * TILE * COLS * 4 <= RINGS, "the sums fit over the rings");
+    constexpr int SMEM_SM = 227 * 1024, SMEM_CTA = SMEM_SM - 1024;
+    const int run_bytes = a.m * RUN_COLUMNS * 2 + (BF16_X ? RUN * COLS * 4 : 0), fixed = RINGS + a.m * 64 + 16;
+    const uint32_t runs = (a.blocks + RUN - 1) / RUN;
+    // Work for most of the GPU out of few rows of W: several warps of a CTA share rows (warps_k), which costs little but
+    // stages the same x against fewer rows; or several CTAs of a cluster do (split), which stages each column of x once but
+    // waits for the cluster twice.  One to four rows of x take the first, more the second; what is still too little takes
+    // the other as well.  (1 x 4096 x 4096: 5.8 us with four warps, 7.5 with four CTAs, 11.5 with neither;
+    // 16 x 4096 x 4096: 15.5, 11.0, 24.8.)
+    constexpr uint32_t ENOUGH = 120;
+    uint32_t split = 1;
+    a.warps_k = 1;
+    auto ctas = [&] { const uint32_t rows = GEMV_WARPS * TILE / a.warps_k; return (a.n + rows - 1) / rows * split; };
+    auto share_warps = [&] { while (ctas() < ENOUGH && a.warps_k < GEMV_WARPS && (uint32_t)a.warps_k * split < runs) a.warps_k *= 2; };
+    auto share_ctas = [&](uint32_t least) { while (ctas() < ENOUGH && split < 8 && split * 2 * (uint32_t)a.warps_k * least <= runs) split *= 2; };
+    if (a.m <= 4) { share_warps(); share_ctas(2); }
+    else { share_ctas(1); share_warps(); }
+    // A chunk of x is whole rounds of the warps that share rows, so that each goes on with its runs from chunk to chunk.  It
+    // leaves room for two CTAs a multiprocessor if a round fits then.
+    int fit = ((SMEM_SM - 4096) / 2 - fixed) / run_bytes;
+    if (fit < a.warps_k) fit = (SMEM_CTA - fixed) / run_bytes;
+    static_assert((SMEM_CTA - RINGS - 8 * NT * 64 - 16) / (8 * NT * RUN_COLUMNS * 2 + RUN * COLS * 4) >= 1, "one run of all rows always fits");
+    while (a.warps_k > fit) a.warps_k /= 2;
+    const uint32_t rows = GEMV_WARPS * TILE / a.warps_k, row_groups = (a.n + rows - 1) / rows;
+    const int runs_of_cta = (int)((runs + split - 1) / split), most = fit / a.warps_k * a.warps_k;
+    a.chunk_runs = runs_of_cta < most ? runs_of_cta : most;
+    const int bytes = fixed + a.chunk_runs * run_bytes;
+    // room for shared memory is asked for once per kernel and device: a bit of `raised` each
+    static std::atomic<uint64_t> raised{0};
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return FBSR_ERR_CUDA;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device >= 64 || !(raised.load(std::memory_order_relaxed) & bit)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_CTA) != cudaSuccess) return FBSR_ERR_CUDA;
+        raised.fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(row_groups, split);
+    config.blockDim = dim3(GEMV_THREADS);
+    config.dynamicSmemBytes = (size_t)bytes;
+    config.stream = stream;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = 1; cluster.val.clusterDim.y = split; cluster.val.clusterDim.z = 1;
+    config.attrs = &cluster;
+    config.numAttrs = split > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&config, kernel, a) != cudaSuccess) return FBSR_ERR_CUDA;
     count_launch();
     return cudaGetLastError() == cudaSuccess ? FBSR_OK : FBSR_ERR_CUDA;
 }
 
-template <bool BF16_X>
+template <bool BF16_X, bool BF16_S, int COUNT>
 int launch_rows(const GemvArgs& a, cudaStream_t stream)
 {
-    if (a.m <= 8) return launch<BF16_X, 1, 1>(a, stream);
-    if (a.m <= 16) return launch<BF16_X, 2, 1>(a, stream);
-    return launch<BF16_X, 4, 1>(a, stream);
+    if (a.m == 1) return launch<BF16_X, BF16_S, COUNT, true, 1, 3>(a, stream);
+    if (a.m <= 8) return launch<BF16_X, BF16_S, COUNT, false, 1, 2>(a, stream);
+    if (a.m <= 16) return launch<BF16_X, BF16_S, COUNT, false, 2, 2>(a, stream);
+    return launch<BF16_X, BF16_S, COUNT, false, 4, 2>(a, stream);
 }
+
+typedef int (*launch_fn)(const GemvArgs&, cudaStream_t);
+// [x is bfloat16][scales are bfloat16][group 32, 64, 128]
+const launch_fn kLaunch[2][2][3] = {
+    {{launch_rows<false, false, 4>, launch_rows<false, false, 2>, launch_rows<false, false, 1>},
+     {launch_rows<false, true, 4>, launch_rows<false, true, 2>, launch_rows<false, true, 1>}},
+    {{launch_rows<true, false, 4>, launch_rows<true, false, 2>, launch_rows<true, false, 1>},
+     {launch_rows<true, true, 4>, launch_rows<true, true, 2>, launch_rows<true, true, 1>}}};
 
 inline bool off(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
@@ -289,15 +455,16 @@ extern "C" int fbsr_gemv_w4(const void* x, int x_fmt, int64_t ldx, size_t m, con
     a.codes = codes; a.scales = static_cast<const uint8_t*>(scales);
     a.ldx = ldx; a.ldy = ldy;
     a.n = (uint32_t)n; a.k = (uint32_t)k; a.blocks = (uint32_t)(fbsr_w4_padded(k) / W4_BLOCK);
-    a.block_scale_bytes = W4_BLOCK / (uint32_t)group * scale_bytes;
-    a.row_scale_bytes = a.blocks * a.block_scale_bytes;
-    a.out_fmt = out_fmt; a.scale_bf16 = scale_fmt == FBSR_SCALE_BF16;
-    if (off(x, 2) || off(codes, 16) || off(scales, a.block_scale_bytes)) return FBSR_ERR_ALIGNMENT;
+    const uint32_t block_scale_bytes = W4_BLOCK / (uint32_t)group * scale_bytes;
+    a.row_scale_bytes = a.blocks * block_scale_bytes;
+    a.out_fmt = out_fmt;
+    const launch_fn launch_m = kLaunch[x_fmt == FBSR_BF16][scale_fmt == FBSR_SCALE_BF16][group == 32 ? 0 : group == 64 ? 1 : 2];
+    if (off(x, 2) || off(codes, 16) || off(scales, block_scale_bytes)) return FBSR_ERR_ALIGNMENT;
     for (size_t at = 0; at < m; at += GEMV_MAX_M) {
         a.x = static_cast<const uint16_t*>(x) + (int64_t)at * ldx;
         a.y = static_cast<char*>(y) + (int64_t)at * ldy * (int64_t)out_bytes;
         a.m = (int)(m - at < (size_t)GEMV_MAX_M ? m - at : (size_t)GEMV_MAX_M);
-        const int rc = x_fmt == FBSR_BF16 ? launch_rows<true>(a, stream) : launch_rows<false>(a, stream);
+        const int rc = launch_m(a, stream);
         if (rc != FBSR_OK) return rc;
     }
     return FBSR_OK;

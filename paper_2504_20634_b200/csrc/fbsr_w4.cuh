@@ -32,11 +32,28 @@ __device__ __forceinline__ uint32_t e2m1_pair_to_half2(uint32_t byte)
     return r;
 }
 
+// Eight codes (a word of the stored order) to four pairs of binary16 values.
+__device__ __forceinline__ void e2m1_word_to_half2(uint32_t word, uint32_t (&h)[4])
+{
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(word));
+}
+
 // 2^(byte - 127) of a power-of-two scale; 255 is the NaN scale.
 __device__ __forceinline__ float e8m0_value(uint32_t byte)
 {
     const uint32_t p = byte << 23;
     return __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7FC00000u : p);
+}
+
+// The same for the two low bytes, as a pair of bfloat16 (which holds every one of these values).
+__device__ __forceinline__ uint32_t e8m0_pair_to_bf16x2(uint32_t bytes)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.bf16x2.ue8m0x2 %0, lo;\n\t}" : "=r"(r) : "r"(bytes));
+    return r;
 }
 
 }  // namespace fbsr
