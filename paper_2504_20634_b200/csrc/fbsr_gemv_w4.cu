@@ -385,15 +385,8 @@ int launch(GemvArgs a, cudaStream_t stream)
     const int runs_of_cta = (int)((runs + split - 1) / split), most = fit / a.warps_k * a.warps_k;
     a.chunk_runs = runs_of_cta < most ? runs_of_cta : most;
     const int bytes = fixed + a.chunk_runs * run_bytes;
-    // room for shared memory is asked for once per kernel and device: a bit of `raised` each
-    static std::atomic<uint64_t> raised{0};
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return FBSR_ERR_CUDA;
-    const uint64_t bit = 1ull << (device & 63);
-    if (device >= 64 || !(raised.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_CTA) != cudaSuccess) return FBSR_ERR_CUDA;
-        raised.fetch_or(bit, std::memory_order_relaxed);
-    }
+    static std::atomic<uint64_t> allowed{0};
+    if (int rc = allow_shared_memory((const void*)kernel, SMEM_CTA, allowed)) return rc;
     cudaLaunchConfig_t config{};
     config.gridDim = dim3(row_groups, split);
     config.blockDim = dim3(GEMV_THREADS);

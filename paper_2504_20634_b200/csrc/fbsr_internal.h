@@ -1,5 +1,6 @@
 // Host-side plumbing shared by the translation units of libfbsr.so (not part of the public ABI).
 #pragma once
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -51,6 +52,19 @@ constexpr int MAX_SLOW_GRID = 148 * 8;      // CTAs of the general kernel; also 
     int dispatch_qat_adamw_##fmt(const CallArgs&);
 FBSR_DECLARE_DISPATCH(0) FBSR_DECLARE_DISPATCH(1) FBSR_DECLARE_DISPATCH(2) FBSR_DECLARE_DISPATCH(3) FBSR_DECLARE_DISPATCH(4)
 #undef FBSR_DECLARE_DISPATCH
+
+// Lets a kernel have `bytes` of dynamic shared memory: asked for once per kernel and device, `done` holding a bit for each
+// device that has been asked.  FBSR_OK (0) or FBSR_ERR_CUDA (4).
+inline int allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64_t>& done)
+{
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return 4;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return 4;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return 0;
+}
 
 void count_launch();                         // bumps the counter behind fbsr_launch_count()
 

@@ -190,6 +190,56 @@ def test_8bit_state_codes_and_scales(variant, k, grad, misalign):
             gu.assert_codes_equal(got, code, "%s of tensor %d" % ("v" if positive else "m", i))
 
 
+@pytest.mark.parametrize("misalign", [4, 8, 16])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", ["fp32", "bf16"])
+def test_alignments_between_element_and_vector(misalign, bits, grad):
+    """Pointers that allow 16-byte copies, vector stores, or one of the two, give what aligned tensors give."""
+    t, u = (make(SIZES, seed=40, bits=bits, grad=grad, misalign=x) for x in (misalign, 0))
+    for x in (t, u):
+        fbsr.fbsr_adamw_multi(x["table"], "src", 4, 9, **HYPER)
+    for q in ("w", "m", "v", "lp", "ms", "vs"):
+        for a, b in zip(t[q], u[q]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), q
+
+
+def test_roots_and_quotients_of_the_8bit_step_are_rounded_correctly():
+    """One element a block is not zero: its scale is the root of the new second moment over 448; with c1 a power of two and
+    no weight before, the new weight is the quotient."""
+    blocks = 1 << 16
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    g = torch.zeros(blocks, 256, device="cuda")
+    g[:, 3] = torch.randn(blocks, device="cuda", generator=gen) * torch.exp2(torch.rand(blocks, device="cuda", generator=gen) * 60 - 40)
+    n = g.numel()
+    z = lambda dt, k=n: torch.zeros(k, dtype=dt, device="cuda")  # noqa: E731
+    w, ms, vs = z(torch.float32), z(torch.float32, blocks), z(torch.float32, blocks)
+    t = fbsr.FbsrAdamwTensors([w], [g.view(-1)], [z(torch.uint8)], [z(torch.uint8)], None, m_scale=[ms], v_scale=[vs])
+    fbsr.fbsr_adamw_multi(t, "rtne", 1, 0, lr=2.0 ** -10, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=10 ** 6)
+    f = np.float32
+    x = host(g[:, 3])
+    v = (f(1 - 0.999) * x) * x
+    root = np.sqrt(v)
+    assert np.array_equal(host(vs), np.maximum(root * (f(1) / f(448)), f(2.0 ** -126)))
+    q = (f(1 - 0.9) * x) / (root + f(1e-8))                  # c2 is one by then
+    assert np.array_equal(host(w.view(blocks, 256)[:, 3]), -q * f(2.0 ** -10))
+
+
+def test_second_moments_outside_the_fast_root():
+    """Very small and very large gradients: the moments' scales and signs hold, an overflowing second moment moves nothing."""
+    n = 1024
+    g = torch.zeros(n, device="cuda")
+    g[0], g[1], g[256], g[512], g[513] = 1e-18, -1e-22, 3e38, -2e19, 1e-3
+    z = lambda dt, k=n: torch.zeros(k, dtype=dt, device="cuda")  # noqa: E731
+    w, m, v, ms, vs = z(torch.float32) + 0.5, z(torch.uint8), z(torch.uint8), z(torch.float32, 4), z(torch.float32, 4)
+    t = fbsr.FbsrAdamwTensors([w], [g], [m], [v], None, m_scale=[ms], v_scale=[vs])
+    fbsr.fbsr_adamw_multi(t, "rtne", 1, 0, **dict(HYPER, weight_decay=0.0, step=1))
+    assert torch.isfinite(w).all() and torch.isfinite(ms).all() and torch.isfinite(vs).all()
+    assert int(m[1]) == 0x80 and int(m[256]) == 0x7E and int(m[512]) == 0xFE       # -1e-22 beside 1e-18 rounds to a signed zero
+    assert int(v[256]) == 0x7E and float(w[256]) == 0.5 and float(w[512]) == 0.5
+    f = np.float32
+    assert float(vs[0]) == np.sqrt((f(1 - 0.999) * f(1e-18)) * f(1e-18)) * (f(1) / f(448))
+
+
 def test_fresh_8bit_state_steps_as_binary32_does():
     """From zero state the first step's moments are one product each, the same whatever the state's width."""
     a, b = make((4096, 33), 9, bits=8, fresh=True), make((4096, 33), 9, bits=32, fresh=True)
