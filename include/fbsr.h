@@ -195,7 +195,8 @@ int fbsr_round_mx(const float* src, void* dst, uint8_t* scales, size_t n, int fm
  *   values     NULL, or device, rows x cols of src_fmt at values + r values_ld: the values that the codes stand for, rounded
  *              once to src_fmt (what a forward pass over 4-bit weights multiplies with); must not overlap src
  *   offset     a multiple of 128, at most 2^62; element (r, c) has the global index offset + r padded + c for its draw.
- * Rows whose addresses allow it (32 bytes for binary32, 16 for 16-bit) are read and written eight elements at a time. */
+ * At most 2^30 blocks of 128 (FBSR_ERR_TOO_LARGE).  Rows whose addresses allow it (32 bytes for binary32, 16 for 16-bit) are
+ * read and written eight elements at a time. */
 #define FBSR_SCALE_E8M0 0
 #define FBSR_SCALE_BF16 1
 size_t fbsr_w4_padded(size_t cols);

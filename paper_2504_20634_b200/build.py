@@ -26,6 +26,7 @@ SINGLE_UNITS = ["fbsr_api", "fbsr_descriptor", "fbsr_adamw_multi", "fbsr_round_w
 def _units():
     units = [(name + ".o", name + ".cu", []) for name in SINGLE_UNITS]
     units += [("fbsr_adamw_multi_f%d.o" % fmt, "fbsr_adamw_multi.cu", ["-DFBSR_FMT=%d" % fmt]) for fmt in range(5)]
+    units += [("fbsr_round_w4_f%d.o" % t, "fbsr_round_w4.cu", ["-DFBSR_W4_TYPE=%d" % t]) for t in (0, 1, 32)]     # bf16, fp16, fp32
     for group in (2, 6, 5, 3, 1, 0, 4):       # the longest compilations first
         for fmt in range(5):
             if group in (2, 3, 6) and fmt < 2:
