@@ -208,8 +208,8 @@ int fbsr_round_w4(const void* src, int src_fmt, int64_t src_ld, size_t rows, siz
  * quantised weights of Algorithm 1 exist for):  y[i][r] = sum over c < k of x[i][c] value(W[r][c]),
  * value(W[r][c]) = code s.  Each group's products are exact, summed in binary32 and multiplied by s in binary32; groups
  * are added in binary32, in an order that depends on the shapes alone; one rounding to out_fmt at the end.  bfloat16
- * elements of x below 2^-32 of their row's largest finite magnitude are rounded to 2^-40 of it.  NaN and infinities in x
- * and NaN scales go where the formula takes them.
+ * elements of x below 2^-32 of the largest finite magnitude of their 128 columns are rounded to 2^-40 of it, and scales
+ * above 2^100 may overflow before the sum does.  NaN and infinities in x and NaN scales go where the formula takes them.
  *   x        device, m rows of k values of x_fmt (FBSR_BF16 or FBSR_FP16), row i at x + i ldx (elements)
  *   codes, scales, scale_fmt, group   n x k matrix as written by fbsr_round_w4 (its rows x cols); codes 16-byte aligned,
  *            scales aligned to the scales of 128 elements (1 to 8 bytes); codes beyond column k must be zero

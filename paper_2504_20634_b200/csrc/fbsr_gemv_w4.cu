@@ -9,16 +9,23 @@
 // stay exact, scales are applied in binary32.  (The fifth-generation unit would take 128-row tiles from shared memory:
 // the decoded weights would have to be written there and read back, for a product that is far from compute-bound.)
 //
-// A CTA takes 128 rows of W, 16 to a warp, and a range of the columns; up to eight CTAs of a cluster share the columns of
-// the same rows and add their sums over distributed shared memory in a fixed order.  Many rows against a short range of
-// columns keep the work on x small: it is staged once per CTA, m values a column against 128 codes.  Row g of a warp's tile
-// is read by four lanes, 16 bytes each, and lane t's words of the four quarters of a block of 128 columns meet x's elements
-// [32 j + 8 t, + 8): the order of k inside the matrix instruction is the same permutation on both sides.  Four blocks are in
-// flight per warp.
+// A CTA takes up to 128 rows of W, 16 to a warp, and a range of the columns.  Each warp keeps three stages of 16 rows by 512
+// columns on their way through shared memory (two where x is more than a row): enough bytes in flight for the memory's
+// latency without registers.  Row g of the warp's tile is read by four lanes, 16 bytes each, and lane t's words of the four
+// quarters of a block of 128 columns meet x's elements [32 j + 8 t, + 8): the order of k inside the matrix instruction is the
+// same permutation on both sides.  Where the rows are few, warps of a CTA or CTAs of a cluster share the columns of the same
+// rows and add their sums in a fixed order (see launch).
 //
-// x is staged in shared memory in binary16.  bfloat16 rows are first multiplied by the power of two that brings the row's
-// largest finite magnitude to [2^14, 2^15): elements down to 2^-32 of it keep all their 8 bits, smaller ones are rounded
-// to 2^-40 of it, far below the rounding of the binary32 sums; the sum is multiplied back at the end.
+// x is staged in shared memory in binary16, once per CTA.  Each block of 128 columns of a bfloat16 row is first multiplied by
+// the power of two that brings its largest finite magnitude to [2^14, 2^15): elements down to 2^-32 of it keep all their 8
+// bits, smaller ones are rounded to 2^-40 of it, far below the rounding of the binary32 sums; the block's sum is multiplied
+// back as it joins the others.
+//
+// Measured, one row of x, bfloat16, groups of 32, on the device: 128000 x 4096 55 us = 5.06 TB/s (0.77 of the measured copy
+// rate), 28672 x 8192 31 us, 4096 x 11008 9.6 us, 4096 x 4096 5.8 us, 1024 x 4096 4.0 us; eight rows by 11008 x 4096 14.3 us.
+// What bounds the large ones is issue latency, not memory (16 warps a multiprocessor, 111 instructions for a 16 x 128 block,
+// 51 % of the issue slots): 24 warps with half the stage gained 3 % there and lost 14 % at 8192 columns; two tiles a warp, bulk
+// copies a row at a time, codes through registers and blocks without the way out between them were slower.
 #include <atomic>
 
 #include <cooperative_groups.h>
@@ -65,25 +72,36 @@ __device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// The COUNT scales of a block (SB bytes at p, in shared memory) as numbers.
-template <bool BF16_S, int COUNT>
-__device__ __forceinline__ void block_scales(const unsigned char* p, float (&s)[COUNT])
-{
-    constexpr int SB = COUNT * (BF16_S ? 2 : 1);
-    uint32_t w[SB == 8 ? 2 : 1];
-    if constexpr (SB == 8) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        w[0] = v.x; w[1] = v.y;
-    } else if constexpr (SB == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
-    else if constexpr (SB == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
-    else w[0] = *p;
+// A row's scales of a run (SB bytes a block) out of shared memory, and those of block d as numbers.
+template <int SB> struct RunScales {
+    uint32_t w[SB];                              // RUN SB bytes
+    __device__ __forceinline__ void load(const unsigned char* p)
+    {
+        static_assert(RUN == 4, "a word holds one, two or four bytes of each block");
+        if constexpr (SB == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
+        if constexpr (SB == 2) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
+        if constexpr (SB >= 4) {
 #pragma unroll
-    for (int i = 0; i < COUNT; i += 2) {         // scales i and i + 1 as bfloat16
-        const uint32_t pair = BF16_S ? w[i / 2] : e8m0_pair_to_bf16x2(i ? w[0] >> 16 : w[0]);
-        s[i] = __uint_as_float(pair << 16);
-        if constexpr (COUNT > 1) s[i + 1] = __uint_as_float(pair & 0xFFFF0000u);
+            for (int i = 0; i < SB; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i);
+                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+            }
+        }
     }
-}
+    template <bool BF16_S, int COUNT>
+    __device__ __forceinline__ void values(int d, float (&s)[COUNT]) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; i += 2) {     // scales i and i + 1 as bfloat16
+            uint32_t pair;
+            if constexpr (BF16_S && COUNT == 1) pair = w[d / 2] >> (16 * (d & 1));
+            else if constexpr (BF16_S) pair = w[(d * COUNT + i) / 2];
+            else pair = e8m0_pair_to_bf16x2(w[(d * COUNT + i) / 4] >> (8 * ((d * COUNT + i) & 3)));
+            s[i] = __uint_as_float(pair << 16);
+            if constexpr (COUNT > 1) s[i + 1] = __uint_as_float(pair & 0xFFFF0000u);
+        }
+    }
+};
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(unsigned char* smem_dst, const uint8_t* gmem_src)
@@ -187,7 +205,8 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
     constexpr int STEP = ONE ? 2 : 1;            // of the four sums of a lane, those of column 0 are the first and the third
     constexpr int STAGE = TILE * (ROW_PITCH + RUN * SB);
     extern __shared__ __align__(16) unsigned char smem[];
-    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), g = lane >> 2, t = lane & 3;
+    const uint32_t lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), g = (int)lane >> 2, t = (int)lane & 3;
     const int rows = GEMV_WARPS * TILE / a.warps_k, warp_row = warp / a.warps_k, warp_k = warp % a.warps_k;
     const uint32_t row0 = blockIdx.x * rows + warp_row * TILE;
     const int stride = a.chunk_runs * (RUN * W4_BLOCK) + 32;       // elements: 64 bytes more, so that two rows meet different banks
@@ -200,35 +219,47 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
     const uint32_t runs = (a.blocks + RUN - 1) / RUN;
     const uint32_t q_begin = (uint32_t)((uint64_t)runs * blockIdx.y / gridDim.y), q_end = (uint32_t)((uint64_t)runs * (blockIdx.y + 1) / gridDim.y);
 
-    // Each warp fills its own ring, sixteen lanes to a row of 256 bytes; odd rows have neighbouring 64 bytes exchanged so that
+    // Each warp fills its own ring, neighbouring lanes to a row; odd rows have neighbouring 64 bytes exchanged so that
     // the lanes that read two rows together meet different banks.  The rows' scales follow as words.  Rows beyond the matrix
     // are left as they are: what comes of them is dropped.
     const uint32_t tile_rows = row0 >= a.n ? 0u : min((uint32_t)TILE, a.n - row0), pitch = a.blocks * W4_BLOCK_BYTES;
-    const uint8_t* copy_src = a.codes + (uint64_t)(row0 + (lane >> 4)) * pitch + (lane & 15) * 16;
-    const uint32_t copy_dst = (lane >> 4) * ROW_PITCH + ((lane & 15) ^ ((lane >> 4) << 2)) * 16;
-    const bool scales_by_4 = a.row_scale_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0;
+    // warp-uniform addresses, and what the lane adds to them
+    const uint8_t* codes = a.codes + (uint64_t)row0 * pitch;
+    const uint8_t* scales = a.scales + (uint64_t)row0 * a.row_scale_bytes;
+    constexpr uint32_t ROW_LANES = ROW_PITCH / 16, ROWS_AT_ONCE = 32 / ROW_LANES;  // lanes to a row's codes
+    const uint32_t lane_row = lane / ROW_LANES, lane_piece = lane % ROW_LANES;
+    const uint32_t copy_from = lane_row * pitch + lane_piece * 16;
+    const uint32_t copy_to = lane_row * ROW_PITCH + (lane_piece ^ ((lane_row & 1) << 2)) * 16;
+    constexpr uint32_t WORDS = RUN * SB / 4 > 0 ? RUN * SB / 4 : 1;                // of a row's scales of a stage
+    const uint32_t scale_from = lane / WORDS * a.row_scale_bytes + lane % WORDS * 4;
+    const bool scales_by_4 = RUN * SB % 4 == 0 && a.row_scale_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0;
     auto issue = [&](uint32_t q, int slot) {
         if (q < q_end) {
             unsigned char* to = ring + slot * STAGE;
-            const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
-            if ((uint32_t)(lane & 15) < here * 4) {
-#pragma unroll
-                for (int r = 0; r < TILE; r += 2)
-                    if (r + (lane >> 4) < tile_rows) copy_async<16>(to + copy_dst + r * ROW_PITCH, copy_src + (uint64_t)r * pitch + q * ROW_PITCH);
-            }
-            constexpr int WORDS = RUN * SB / 4;                    // of a row's scales of this stage
             unsigned char* scales_to = to + TILE * ROW_PITCH;
-            const uint8_t* from = a.scales + q * (RUN * SB);
-            if (scales_by_4) {
+            const uint8_t* from = codes + q * ROW_PITCH;
+            const uint8_t* scales_at = scales + q * (RUN * SB);
+            if (tile_rows == TILE && q * RUN + RUN <= a.blocks && scales_by_4) {   // a whole stage
 #pragma unroll
-                for (int i = 0; i < (TILE * WORDS + 31) / 32; ++i) {
-                    const uint32_t item = i * 32 + lane, row = item / WORDS, word = item % WORDS;
-                    if (row < tile_rows && word * 4 < here * SB)
-                        copy_async<4>(scales_to + item * 4, from + (uint64_t)(row0 + row) * a.row_scale_bytes + word * 4);
+                for (int r = 0; r < TILE; r += ROWS_AT_ONCE) copy_async<16>(to + copy_to + r * ROW_PITCH, from + r * pitch + copy_from);
+#pragma unroll
+                for (int i = 0; i < TILE * WORDS; i += 32)
+                    if (TILE * WORDS >= 32 || lane < TILE * WORDS)
+                        copy_async<4>(scales_to + (i + lane) * 4, scales_at + i / WORDS * a.row_scale_bytes + scale_from);
+            } else {
+                const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
+#pragma unroll
+                for (int r = 0; r < TILE; r += ROWS_AT_ONCE)
+                    if (lane_piece < here * 4 && r + lane_row < tile_rows)
+                        copy_async<16>(to + copy_to + r * ROW_PITCH, from + r * pitch + copy_from);
+                if (scales_by_4) {
+#pragma unroll
+                    for (int i = 0; i < TILE * WORDS; i += 32)
+                        if ((i + lane) / WORDS < tile_rows && lane % WORDS * 4 < here * SB)
+                            copy_async<4>(scales_to + (i + lane) * 4, scales_at + i / WORDS * a.row_scale_bytes + scale_from);
+                } else if (lane < tile_rows) {                     // rows of scales off the word grid: byte by byte
+                    for (uint32_t i = 0; i < here * SB; ++i) scales_to[lane * (RUN * SB) + i] = __ldg(scales_at + lane * a.row_scale_bytes + i);
                 }
-            } else if (lane < tile_rows) {                         // rows of scales off the word grid: byte by byte
-                for (uint32_t i = 0; i < here * SB; ++i)
-                    scales_to[lane * (RUN * SB) + i] = __ldg(from + (uint64_t)(row0 + lane) * a.row_scale_bytes + i);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -262,6 +293,9 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
             const unsigned char* codes_of[2] = {from + g * ROW_PITCH + (g & 1) * 64 + t * 16, from + g * ROW_PITCH + ((g & 1) ^ 1) * 64 + t * 16};
             const unsigned char* scales_of = from + TILE * ROW_PITCH + g * (RUN * SB);
             const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
+            RunScales<SB> scales_of_row[2];      // blocks that the last run of a row lacks: not used
+            scales_of_row[0].load(scales_of);
+            scales_of_row[1].load(scales_of + 8 * (RUN * SB));
 #pragma unroll
             for (int d = 0; d < RUN; ++d) {
                 if (d >= here) break;
@@ -271,7 +305,7 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     code[h] = *reinterpret_cast<const uint4*>(codes_of[d & 1] + 8 * h * ROW_PITCH + (d & ~1) * W4_BLOCK_BYTES);
-                    block_scales<BF16_S, COUNT>(scales_of + 8 * h * (RUN * SB) + d * SB, s[h]);
+                    scales_of_row[h].template values<BF16_S, COUNT>(d, s[h]);
                 }
 #pragma unroll
                 for (int i = 0; i < COUNT; ++i) {
@@ -365,8 +399,8 @@ int launch(GemvArgs a, cudaStream_t stream)
     // Work for most of the GPU out of few rows of W: several warps of a CTA share rows (warps_k), which costs little but
     // stages the same x against fewer rows; or several CTAs of a cluster do (split), which stages each column of x once but
     // waits for the cluster twice.  One to four rows of x take the first, more the second; what is still too little takes
-    // the other as well.  (1 x 4096 x 4096: 5.8 us with four warps, 7.5 with four CTAs, 11.5 with neither;
-    // 16 x 4096 x 4096: 15.5, 11.0, 24.8.)
+    // the other as well.  (4096 x 4096, one row of x: 5.8 us with four warps sharing, 7.5 with four CTAs, 11.5 with neither;
+    // sixteen rows: 15.5, 11.0, 24.8.)
     constexpr uint32_t ENOUGH = 120;
     uint32_t split = 1;
     a.warps_k = 1;
