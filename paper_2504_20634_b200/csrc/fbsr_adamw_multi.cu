@@ -187,13 +187,13 @@ __device__ __forceinline__ float root_in_range(float v)
     return __fmaf_rn(__fmaf_rn(-g, g, v), __fmul_rn(0.5f, y), g);
 }
 
-// m / d for d = 0 (NaN) or d >= 2^-126.  d beyond 2^126 (an infinite second moment) counts as 2^126, whose quotient moves no weight; quotients
+// m / d for d = 0 (NaN) or 2^-126 <= d <= 2^126 or an infinite d (an overflowing second moment: zero for finite m).  Quotients
 // whose residual m - q d is below binary32's range (m below about 2^-100) may be one unit off.
 __device__ __forceinline__ float quotient(float m, float d)
 {
     float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(d));          // zero for an infinite d, and zero it stays
     asm("min.NaN.f32 %0, %0, 0f7E800000;" : "+f"(d));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(d));
     y = __fmaf_rn(y, __fmaf_rn(-d, y, 1.0f), y);
     const float q = __fmul_rn(m, y);
     return __fmaf_rn(__fmaf_rn(-d, q, m), y, q);
@@ -203,9 +203,11 @@ __device__ __forceinline__ void roots8(const float (&v)[8], float (&r)[8])
 {
     float low = v[0], high = v[0];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        r[c] = root_in_range(v[c]);
-        low = fminf(low, v[c]); high = fmaxf(high, v[c]);
+    for (int c = 0; c < 8; ++c) r[c] = root_in_range(v[c]);
+#pragma unroll
+    for (int c = 0; c < 8; c += 2) {
+        asm("min.f32 %0, %0, %1, %2;" : "+f"(low) : "f"(v[c]), "f"(v[c + 1]));
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(high) : "f"(v[c]), "f"(v[c + 1]));
     }
     if (!(low >= 0x1p-96f && high <= 0x1p126f)) {
 #pragma unroll
@@ -219,7 +221,7 @@ __device__ __forceinline__ float row_amax(const float (&x)[8])
 {
     float m = 0.0f;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) m = fmaxf(m, fabsf(x[c]));                       // ignores NaN
+    for (int c = 0; c < 8; c += 2) asm("max.abs.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(x[c]), "f"(x[c + 1]));      // ignores NaN
     const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m));
     if (all < 0x7F800000u) return __uint_as_float(all);
     m = 0.0f;                                    // an infinity in the row (rare, the same for all lanes)
@@ -251,7 +253,13 @@ __device__ __forceinline__ float round_state(const float (&x)[8], const uint4& d
 #pragma unroll
             for (int c = 0; c < 8; ++c) t[c] = max(t[c], min(__float_as_uint(x[c]), 1u << (Row<E4M3>::SH0 + Row<E4M3>::L)));
         }
-        pack_row_fast<E4M3>(t, y, packed);
+        if constexpr (POSITIVE) {                // no signs to take along
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                packed[j] = __byte_perm(__byte_perm(t[4 * j], t[4 * j + 1], 0x7373), __byte_perm(t[4 * j + 2], t[4 * j + 3], 0x7373), 0x5410);
+        } else {
+            pack_row_fast<E4M3>(t, y, packed);
+        }
     } else {
         uint32_t n[8];
 #pragma unroll
@@ -532,7 +540,7 @@ adamw_multi_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_con
             if constexpr (FMT == BF16) {         // beyond M too, which a draw could carry past the exponent
                 float over = 0.0f;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) over = fmaxf(over, fabsf(w[c]));
+                for (int c = 0; c < 8; c += 2) asm("max.abs.f32 %0, %0, %1, %2;" : "+f"(over) : "f"(w[c]), "f"(w[c + 1]));
                 redo |= over > __uint_as_float(0x7F7F0000u);
             }
             if (!redo) {

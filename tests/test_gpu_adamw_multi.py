@@ -236,7 +236,8 @@ def test_second_moments_outside_the_fast_root():
     assert torch.isfinite(w).all() and torch.isfinite(ms).all() and torch.isfinite(vs).all()
     # -1e-22 beside 1e-18 is -0.0448 = -1.43 2^-5 in units of the scale: exponent field 2, 3.5 eighths (to the nearest, 3), signed
     assert int(m[1]) == 0x93 and int(m[256]) == 0x7E and int(m[512]) == 0xFE
-    assert int(v[256]) == 0x7E and float(w[256]) == 0.5 and float(w[512]) == 0.5
+    # (1e-3 3e38) 3e38 overflows, (1e-3 2e19) 2e19 = 4e35 does not: its weight takes the first step's lr
+    assert int(v[256]) == 0x7E and float(w[256]) == 0.5 and abs(float(w[512]) - 0.501) < 1e-6
     f = np.float32
     assert float(vs[0]) == np.sqrt((f(1 - 0.999) * f(1e-18)) * f(1e-18)) * (f(1) / f(448))
 
