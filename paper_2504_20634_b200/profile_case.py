@@ -17,7 +17,9 @@ from paper_2504_20634_b200 import workloads
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--op", default="round", choices=["round", "sgd", "adam", "accumulate", "stats", "bits", "lp", "mx", "desc", "qat", "qat_adamw"])
+    ap.add_argument("--op", default="round", choices=["round", "sgd", "adam", "accumulate", "stats", "bits", "lp", "mx", "desc", "qat", "qat_adamw",
+                                                        "adamw32", "adamw8", "round_w4", "gemv_w4"])
+    ap.add_argument("--rows", type=int, default=1, help="rows of x for --op gemv_w4")
     ap.add_argument("--src-fmt", default="bf16", help="source format for --op lp")
     ap.add_argument("--fmt", default="bf16")
     ap.add_argument("--variant", default="srf")
@@ -63,6 +65,32 @@ def main():
         bytes_per_elem = 20
         run = lambda s: fbsr.fbsr_qat_adamw_step(out, g16, m, v, args.fmt, args.src_fmt, args.variant, args.k, s, 0,
                                                  1e-3, 0.9, 0.95, 1e-8, 0.1, s + 1)
+    elif args.op in ("adamw32", "adamw8"):
+        # one step over three tensors that make up the n parameters; 8-bit state goes with bfloat16 gradients
+        cut = [n // 2, n // 4, n - n // 2 - n // 4]
+        w, m, v = workloads.optimizer_state(n, device=dev)
+        g = workloads.optimizer_grad(n, 1, device=dev)
+        out = torch.empty(n, dtype=fbsr.CODE_DTYPE[base_fmt], device=dev)
+        more = {}
+        if args.op == "adamw8":
+            g, m, v = g.bfloat16(), torch.zeros(n, dtype=torch.uint8, device=dev), torch.zeros(n, dtype=torch.uint8, device=dev)
+            more = {name: [torch.zeros(-(-c // 256), device=dev) for c in cut] for name in ("m_scale", "v_scale")}
+        table = fbsr.FbsrAdamwTensors(*(list(t.split(cut)) for t in (w, g, m, v, out)), fmt=args.fmt, **more)
+        bytes_per_elem = (28 if args.op == "adamw32" else 14) + code_bytes
+        run = lambda s: fbsr.fbsr_adamw_multi(table, args.variant, args.k, s, 1e-4, 0.9, 0.999, 1e-8, 0.1, s)
+    elif args.op in ("round_w4", "gemv_w4"):
+        # a matrix of 4096 columns, groups of 32 with power-of-two scales
+        w = (torch.randn(n, device=dev) * 0.02).view(-1, 4096)
+        values = torch.empty_like(w)
+        codes, scales = fbsr.fbsr_round_w4(w, args.variant, args.k, 1, values=values)
+        if args.op == "round_w4":
+            bytes_per_elem = 8.5 + 1.0 / 32
+            run = lambda s: fbsr.fbsr_round_w4(w, args.variant, args.k, s, values=values, out=codes, scales=scales)
+        else:
+            x = torch.randn(args.rows, 4096, device=dev).bfloat16()
+            y = torch.empty(args.rows, w.shape[0], device=dev)
+            bytes_per_elem = 0.5 + 1.0 / 32
+            run = lambda s: fbsr.fbsr_gemv_w4(x, codes, scales, out=y)
     elif args.op == "qat":
         # last line of Algorithm 1 with the 16-bit sum: 8-bit weights in place, 16-bit updates: 4 B/element
         fbsr.fbsr_round(x.mul(2.0 ** -18).clamp_(-3, 3), base_fmt, "rtne", 1, seed=0, out=out)
