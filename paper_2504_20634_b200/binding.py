@@ -437,6 +437,7 @@ W4_SCALE_DTYPE = {"e8m0": torch.uint8, "bf16": torch.bfloat16}
 
 _SOURCES = (torch.float32, torch.bfloat16, torch.float16)
 _HALF = (torch.bfloat16, torch.float16)
+_OUT = (None,) + _SOURCES
 _HERE_ALREADY = contextlib.nullcontext()
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
@@ -513,10 +514,14 @@ def fbsr_gemv_w4(x, codes, scales, group=32, out=None, out_dtype=None):
     if scales.shape != (n, 2 * half_row // max(group, 1)) or scales.get_device() != device or not scales.is_contiguous():
         raise ValueError("scales must be a contiguous tensor of shape (%d, %d) on %s" % (n, 2 * half_row // max(group, 1), x.device))
     if out is None:
+        if out_dtype not in _OUT:
+            raise TypeError("out_dtype must be one of %s" % ", ".join(map(str, _SOURCES)))
         out = x.new_empty((m, n), dtype=out_dtype)
-    elif out.shape != (m, n) or out.get_device() != device or out_dtype not in (None, out.dtype):
-        raise ValueError("out must have shape (%d, %d) on %s and the dtype asked for" % (m, n, x.device))
-    py, ldy = _matrix(out, _SOURCES, "out")
+        py, ldy = out.data_ptr(), n
+    else:
+        if out.shape != (m, n) or out.get_device() != device or out_dtype not in (None, out.dtype):
+            raise ValueError("out must have shape (%d, %d) on %s and the dtype asked for" % (m, n, x.device))
+        py, ldy = _matrix(out, _SOURCES, "out")
     with _on(device):
         status = _L.fbsr_gemv_w4(px, SOURCE_TYPE[x.dtype], ldx, m, codes.data_ptr(), scales.data_ptr(), scale_fmt, group, n, k, py,
                                  SOURCE_TYPE[out.dtype], ldy, _raw_stream(device))
