@@ -9,23 +9,25 @@
 // stay exact, scales are applied in binary32.  (The fifth-generation unit would take 128-row tiles from shared memory:
 // the decoded weights would have to be written there and read back, for a product that is far from compute-bound.)
 //
-// A CTA takes up to 128 rows of W, 16 to a warp, and a range of the columns.  Each warp keeps three stages of 16 rows by 512
-// columns on their way through shared memory (two where x is more than a row): enough bytes in flight for the memory's
-// latency without registers.  Row g of the warp's tile is read by four lanes, 16 bytes each, and lane t's words of the four
-// quarters of a block of 128 columns meet x's elements [32 j + 8 t, + 8): the order of k inside the matrix instruction is the
-// same permutation on both sides.  Where the rows are few, warps of a CTA or CTAs of a cluster share the columns of the same
-// rows and add their sums in a fixed order (see launch).
+// A warp takes tiles of 16 rows of W in runs of 512 columns, of which it keeps two or three on their way through a ring in shared
+// memory: enough bytes in flight for the memory's latency without registers.  Row g of the tile is read by four lanes, 16 bytes
+// each, and lane t's words of the four quarters of a block of 128 columns meet x's elements [32 j + 8 t, + 8): the order of k
+// inside the matrix instruction is the same permutation on both sides.  Two kernels share this.  Where W has many rows and x
+// fits in shared memory, gemv_w4_stream_kernel gives each multiprocessor one CTA of 16 warps that share its rows' runs equally.
+// Elsewhere gemv_w4_kernel gives a warp one tile at a time, and where the rows are few, warps of a CTA or CTAs of a cluster share
+// the columns of the same rows (see launch).  Both add shared sums in a fixed order.
 //
 // x is staged in shared memory in binary16, once per CTA.  Each block of 128 columns of a bfloat16 row is first multiplied by
 // the power of two that brings its largest finite magnitude to [2^14, 2^15): elements down to 2^-32 of it keep all their 8
 // bits, smaller ones are rounded to 2^-40 of it, far below the rounding of the binary32 sums; the block's sum is multiplied
 // back as it joins the others.
 //
-// Measured, one row of x, bfloat16, groups of 32, on the device: 128000 x 4096 55 us = 5.06 TB/s (0.77 of the measured copy
-// rate), 28672 x 8192 31 us, 4096 x 11008 9.6 us, 4096 x 4096 5.8 us, 1024 x 4096 4.0 us; eight rows by 11008 x 4096 14.3 us.
-// What bounds the large ones is issue latency, not memory (16 warps a multiprocessor, 111 instructions for a 16 x 128 block,
-// 51 % of the issue slots): 24 warps with half the stage gained 3 % there and lost 14 % at 8192 columns; two tiles a warp, bulk
-// copies a row at a time, codes through registers and blocks without the way out between them were slower.
+// Measured, one row of x, groups of 32, on the device, W not in L2: 128000 x 4096 50.6 us = 5.51 TB/s (0.84 of the measured copy
+// rate), 28672 x 8192 27.1 us, 4096 x 11008 (groups of 128) 9.0 us, 4096 x 4096 5.8 us, 1024 x 4096 3.9 us; eight rows by 11008 x
+// 4096 11.9 us, by 128000 x 4096 58.7 us.  What bounds the large ones is the latency of the instructions of 16 warps a
+// multiprocessor (105 registers a thread allow no more), 111 of them for a 16 x 128 block of one row of x, 177 of eight: 24 warps
+// with half the run, two tiles a warp, bulk copies a row at a time, codes through registers and blocks without the way out
+// between them were not faster.  The small ones are a launch, x's way to shared memory and one memory latency.
 #include <atomic>
 
 #include <cooperative_groups.h>
@@ -39,7 +41,7 @@ namespace cg = cooperative_groups;
 namespace fbsr {
 namespace {
 
-constexpr int GEMV_WARPS = 8;
+constexpr int GEMV_WARPS = 8, STREAM_WARPS = 16;
 constexpr int GEMV_THREADS = GEMV_WARPS * 32;
 constexpr int GEMV_MAX_M = 32;                   // rows of x a launch takes
 constexpr int RUN = 4;                           // blocks of 128 columns of a stage
@@ -149,10 +151,10 @@ __device__ __forceinline__ uint32_t top_of8(const uint4& v)
 
 // `blocks` blocks of 128 columns of x, from block `first` on, to shared memory as binary16; COLS: rows of x provided for.
 // Sixteen lanes hold a block of a row, eight elements each; up to four such loads are in flight per thread.
-template <bool BF16_X, int COLS>
+template <bool BF16_X, int COLS, int WARPS>
 __device__ __forceinline__ void stage_x(const GemvArgs& a, uint32_t first, uint32_t blocks, __half* xs, int stride, float* factor)
 {
-    constexpr int FLIGHT = 4, LANES = W4_BLOCK / 8, GROUPS = GEMV_THREADS / LANES;
+    constexpr int FLIGHT = 4, LANES = W4_BLOCK / 8, GROUPS = WARPS * 32 / LANES;
     const uint32_t lane = threadIdx.x % LANES, total = blocks * (COLS == 1 ? 1u : (uint32_t)a.m);
     // group i of sixteen threads takes blocks i, i + GROUPS, ... of all rows' blocks
     uint32_t row = 0, block = threadIdx.x / LANES;
@@ -193,6 +195,119 @@ __device__ __forceinline__ void stage_x(const GemvArgs& a, uint32_t first, uint3
     }
 }
 
+// What a lane adds to the warp-uniform addresses of a stage's codes and scales.  Neighbouring lanes read a row; odd rows have
+// neighbouring 64 bytes exchanged so that the lanes that read two rows together meet different banks.  The rows' scales
+// follow as words.  Rows beyond the matrix are left as they are: what comes of them is dropped.
+template <int SB> struct StageCopy {             // SB: bytes of scales of a block
+    static constexpr uint32_t ROW_LANES = ROW_PITCH / 16, ROWS_AT_ONCE = 32 / ROW_LANES;  // lanes to a row's codes
+    static constexpr uint32_t WORDS = RUN * SB / 4 > 0 ? RUN * SB / 4 : 1;                // of a row's scales of a stage
+    uint32_t lane, pitch, row, piece, from, to, scale_from;
+    bool scales_by_4;
+    __device__ __forceinline__ StageCopy(const GemvArgs& a, uint32_t lane_)
+        : lane(lane_), pitch(a.blocks * W4_BLOCK_BYTES), row(lane_ / ROW_LANES), piece(lane_ % ROW_LANES)
+    {
+        from = row * pitch + piece * 16;
+        to = row * ROW_PITCH + (piece ^ ((row & 1) << 2)) * 16;
+        scale_from = lane / WORDS * a.row_scale_bytes + lane % WORDS * 4;
+        scales_by_4 = RUN * SB % 4 == 0 && a.row_scale_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0;
+    }
+    // Run q of the tile whose first row's codes and scales are given.
+    __device__ __forceinline__ void stage(const GemvArgs& a, unsigned char* dst, const uint8_t* codes, const uint8_t* scales, uint32_t q,
+                                          uint32_t tile_rows) const
+    {
+        unsigned char* scales_to = dst + TILE * ROW_PITCH;
+        const uint8_t* codes_at = codes + q * ROW_PITCH;
+        const uint8_t* scales_at = scales + q * (RUN * SB);
+        if (tile_rows == TILE && q * RUN + RUN <= a.blocks && scales_by_4) {       // a whole stage
+#pragma unroll
+            for (int r = 0; r < TILE; r += ROWS_AT_ONCE) copy_async<16>(dst + to + r * ROW_PITCH, codes_at + r * pitch + from);
+#pragma unroll
+            for (int i = 0; i < TILE * WORDS; i += 32)
+                if (TILE * WORDS >= 32 || lane < TILE * WORDS)
+                    copy_async<4>(scales_to + (i + lane) * 4, scales_at + i / WORDS * a.row_scale_bytes + scale_from);
+        } else {
+            const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
+#pragma unroll
+            for (int r = 0; r < TILE; r += ROWS_AT_ONCE)
+                if (piece < here * 4 && r + row < tile_rows) copy_async<16>(dst + to + r * ROW_PITCH, codes_at + r * pitch + from);
+            if (scales_by_4) {
+#pragma unroll
+                for (int i = 0; i < TILE * WORDS; i += 32)
+                    if ((i + lane) / WORDS < tile_rows && lane % WORDS * 4 < here * SB)
+                        copy_async<4>(scales_to + (i + lane) * 4, scales_at + i / WORDS * a.row_scale_bytes + scale_from);
+            } else if (lane < tile_rows) {       // rows of scales off the word grid: byte by byte
+                for (uint32_t i = 0; i < here * SB; ++i) scales_to[lane * (RUN * SB) + i] = __ldg(scales_at + lane * a.row_scale_bytes + i);
+            }
+        }
+    }
+};
+
+// A stage's `here` blocks against x from block x_block0 of shared memory on, into the lane's sums.
+template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int NT>
+__device__ __forceinline__ void run_products(float (&acc)[NT][4], const unsigned char* from, uint32_t here, uint32_t x_block0,
+                                             const __half* const (&x_lane)[NT], const float* factor, int g, int t)
+{
+    constexpr int SB = COUNT * (BF16_S ? 2 : 1), COLS = ONE ? 1 : 8 * NT;
+    constexpr int QUARTERS = 4 / COUNT;          // quarters of a block under one scale
+    constexpr int STEP = ONE ? 2 : 1;            // of the four sums of a lane, those of column 0 are the first and the third
+    const unsigned char* codes_of[2] = {from + g * ROW_PITCH + (g & 1) * 64 + t * 16, from + g * ROW_PITCH + ((g & 1) ^ 1) * 64 + t * 16};
+    const unsigned char* scales_of = from + TILE * ROW_PITCH + g * (RUN * SB);
+    RunScales<SB> scales_of_row[2];      // blocks that the last run of a row lacks: not used
+    scales_of_row[0].load(scales_of);
+    scales_of_row[1].load(scales_of + 8 * (RUN * SB));
+#pragma unroll
+    for (int d = 0; d < RUN; ++d) {
+        if (d >= here) break;
+        const uint32_t x_block = x_block0 + d;
+        uint4 code[2];
+        float s[2][COUNT], sum[NT][4];               // scales and sums of the block
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            code[h] = *reinterpret_cast<const uint4*>(codes_of[d & 1] + 8 * h * ROW_PITCH + (d & ~1) * W4_BLOCK_BYTES);
+            scales_of_row[h].template values<BF16_S, COUNT>(d, s[h]);
+        }
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            float part[NT][4];                       // of the codes under one scale
+#pragma unroll
+            for (int qu = 0; qu < QUARTERS; ++qu) {
+                const int j = i * QUARTERS + qu;
+                uint32_t lo[4], hi[4];
+                e2m1_word_to_half2(word_of(code[0], j), lo);
+                e2m1_word_to_half2(word_of(code[1], j), hi);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 b = *reinterpret_cast<const uint4*>(x_lane[n] + x_block * W4_BLOCK + 32 * j);
+                    if (qu == 0) mma_f16_first(part[n], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
+                    else mma_f16(part[n], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
+                    mma_f16(part[n], lo[2], hi[2], lo[3], hi[3], b.z, b.w);
+                }
+            }
+            float (&into)[NT][4] = BF16_X ? sum : acc;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; c += STEP) {
+                    const float sc = s[c >> 1][i];
+                    into[n][c] = BF16_X && i == 0 ? __fmul_rn(sc, part[n][c]) : __fmaf_rn(sc, part[n][c], into[n][c]);
+                }
+        }
+        if constexpr (BF16_X) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float f[2];
+                if constexpr (ONE) f[0] = factor[x_block];
+                else {
+                    const float2 both = *reinterpret_cast<const float2*>(factor + x_block * COLS + 8 * n + 2 * t);
+                    f[0] = both.x; f[1] = both.y;
+                }
+#pragma unroll
+                for (int c = 0; c < 4; c += STEP) acc[n][c] = __fmaf_rn(f[c & 1], sum[n][c], acc[n][c]);
+            }
+        }
+    }
+}
+
 // BF16_X: x holds bfloat16.  BF16_S, COUNT: scales are bfloat16, COUNT of them in a block of 128.  ONE: x is one row, which
 // column 0 of the sums stands for alone.  NT: groups of 8 rows of x.  STAGES: of each warp's ring.
 template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int NT, int STAGES>
@@ -201,8 +316,6 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
 {
     constexpr int SB = COUNT * (BF16_S ? 2 : 1); // bytes of scales of a block
     constexpr int COLS = ONE ? 1 : 8 * NT;
-    constexpr int QUARTERS = 4 / COUNT;          // quarters of a block under one scale
-    constexpr int STEP = ONE ? 2 : 1;            // of the four sums of a lane, those of column 0 are the first and the third
     constexpr int STAGE = TILE * (ROW_PITCH + RUN * SB);
     extern __shared__ __align__(16) unsigned char smem[];
     const uint32_t lane = threadIdx.x & 31;
@@ -219,49 +332,12 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
     const uint32_t runs = (a.blocks + RUN - 1) / RUN;
     const uint32_t q_begin = (uint32_t)((uint64_t)runs * blockIdx.y / gridDim.y), q_end = (uint32_t)((uint64_t)runs * (blockIdx.y + 1) / gridDim.y);
 
-    // Each warp fills its own ring, neighbouring lanes to a row; odd rows have neighbouring 64 bytes exchanged so that
-    // the lanes that read two rows together meet different banks.  The rows' scales follow as words.  Rows beyond the matrix
-    // are left as they are: what comes of them is dropped.
-    const uint32_t tile_rows = row0 >= a.n ? 0u : min((uint32_t)TILE, a.n - row0), pitch = a.blocks * W4_BLOCK_BYTES;
-    // warp-uniform addresses, and what the lane adds to them
-    const uint8_t* codes = a.codes + (uint64_t)row0 * pitch;
+    const StageCopy<SB> copy(a, lane);
+    const uint32_t tile_rows = row0 >= a.n ? 0u : min((uint32_t)TILE, a.n - row0);
+    const uint8_t* codes = a.codes + (uint64_t)row0 * copy.pitch;
     const uint8_t* scales = a.scales + (uint64_t)row0 * a.row_scale_bytes;
-    constexpr uint32_t ROW_LANES = ROW_PITCH / 16, ROWS_AT_ONCE = 32 / ROW_LANES;  // lanes to a row's codes
-    const uint32_t lane_row = lane / ROW_LANES, lane_piece = lane % ROW_LANES;
-    const uint32_t copy_from = lane_row * pitch + lane_piece * 16;
-    const uint32_t copy_to = lane_row * ROW_PITCH + (lane_piece ^ ((lane_row & 1) << 2)) * 16;
-    constexpr uint32_t WORDS = RUN * SB / 4 > 0 ? RUN * SB / 4 : 1;                // of a row's scales of a stage
-    const uint32_t scale_from = lane / WORDS * a.row_scale_bytes + lane % WORDS * 4;
-    const bool scales_by_4 = RUN * SB % 4 == 0 && a.row_scale_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0;
     auto issue = [&](uint32_t q, int slot) {
-        if (q < q_end) {
-            unsigned char* to = ring + slot * STAGE;
-            unsigned char* scales_to = to + TILE * ROW_PITCH;
-            const uint8_t* from = codes + q * ROW_PITCH;
-            const uint8_t* scales_at = scales + q * (RUN * SB);
-            if (tile_rows == TILE && q * RUN + RUN <= a.blocks && scales_by_4) {   // a whole stage
-#pragma unroll
-                for (int r = 0; r < TILE; r += ROWS_AT_ONCE) copy_async<16>(to + copy_to + r * ROW_PITCH, from + r * pitch + copy_from);
-#pragma unroll
-                for (int i = 0; i < TILE * WORDS; i += 32)
-                    if (TILE * WORDS >= 32 || lane < TILE * WORDS)
-                        copy_async<4>(scales_to + (i + lane) * 4, scales_at + i / WORDS * a.row_scale_bytes + scale_from);
-            } else {
-                const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
-#pragma unroll
-                for (int r = 0; r < TILE; r += ROWS_AT_ONCE)
-                    if (lane_piece < here * 4 && r + lane_row < tile_rows)
-                        copy_async<16>(to + copy_to + r * ROW_PITCH, from + r * pitch + copy_from);
-                if (scales_by_4) {
-#pragma unroll
-                    for (int i = 0; i < TILE * WORDS; i += 32)
-                        if ((i + lane) / WORDS < tile_rows && lane % WORDS * 4 < here * SB)
-                            copy_async<4>(scales_to + (i + lane) * 4, scales_at + i / WORDS * a.row_scale_bytes + scale_from);
-                } else if (lane < tile_rows) {                     // rows of scales off the word grid: byte by byte
-                    for (uint32_t i = 0; i < here * SB; ++i) scales_to[lane * (RUN * SB) + i] = __ldg(scales_at + lane * a.row_scale_bytes + i);
-                }
-            }
-        }
+        if (q < q_end) copy.stage(a, ring + slot * STAGE, codes, scales, q, tile_rows);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     // the first stages are on their way before x is staged
@@ -283,70 +359,14 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
     for (uint32_t q0 = q_begin; q0 < q_end; q0 += a.chunk_runs) {
         const uint32_t q1 = min(q0 + (uint32_t)a.chunk_runs, q_end);
         if (q0 > q_begin) __syncthreads();       // the previous chunk has been read
-        stage_x<BF16_X, COLS>(a, q0 * RUN, (q1 - q0) * RUN, xs, stride, factor);
+        stage_x<BF16_X, COLS, GEMV_WARPS>(a, q0 * RUN, (q1 - q0) * RUN, xs, stride, factor);
         __syncthreads();
         for (uint32_t q = q0 + warp_k; q < q1; q += a.warps_k) {
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
             __syncwarp();                        // this stage has arrived for all lanes, and all have read the one before it
             issue(q + (STAGES - 1) * a.warps_k, next_slot);
-            const unsigned char* from = ring + slot * STAGE;
-            const unsigned char* codes_of[2] = {from + g * ROW_PITCH + (g & 1) * 64 + t * 16, from + g * ROW_PITCH + ((g & 1) ^ 1) * 64 + t * 16};
-            const unsigned char* scales_of = from + TILE * ROW_PITCH + g * (RUN * SB);
-            const uint32_t here = min((uint32_t)RUN, a.blocks - q * RUN);
-            RunScales<SB> scales_of_row[2];      // blocks that the last run of a row lacks: not used
-            scales_of_row[0].load(scales_of);
-            scales_of_row[1].load(scales_of + 8 * (RUN * SB));
-#pragma unroll
-            for (int d = 0; d < RUN; ++d) {
-                if (d >= here) break;
-                const uint32_t x_block = (q - q0) * RUN + d;
-                uint4 code[2];
-                float s[2][COUNT], sum[NT][4];               // scales and sums of the block
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    code[h] = *reinterpret_cast<const uint4*>(codes_of[d & 1] + 8 * h * ROW_PITCH + (d & ~1) * W4_BLOCK_BYTES);
-                    scales_of_row[h].template values<BF16_S, COUNT>(d, s[h]);
-                }
-#pragma unroll
-                for (int i = 0; i < COUNT; ++i) {
-                    float part[NT][4];                       // of the codes under one scale
-#pragma unroll
-                    for (int qu = 0; qu < QUARTERS; ++qu) {
-                        const int j = i * QUARTERS + qu;
-                        uint32_t lo[4], hi[4];
-                        e2m1_word_to_half2(word_of(code[0], j), lo);
-                        e2m1_word_to_half2(word_of(code[1], j), hi);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const uint4 b = *reinterpret_cast<const uint4*>(x_lane[n] + x_block * W4_BLOCK + 32 * j);
-                            if (qu == 0) mma_f16_first(part[n], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
-                            else mma_f16(part[n], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
-                            mma_f16(part[n], lo[2], hi[2], lo[3], hi[3], b.z, b.w);
-                        }
-                    }
-                    float (&into)[NT][4] = BF16_X ? sum : acc;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int c = 0; c < 4; c += STEP) {
-                            const float sc = s[c >> 1][i];
-                            into[n][c] = BF16_X && i == 0 ? __fmul_rn(sc, part[n][c]) : __fmaf_rn(sc, part[n][c], into[n][c]);
-                        }
-                }
-                if constexpr (BF16_X) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float f[2];
-                        if constexpr (ONE) f[0] = factor[x_block];
-                        else {
-                            const float2 both = *reinterpret_cast<const float2*>(factor + x_block * COLS + 8 * n + 2 * t);
-                            f[0] = both.x; f[1] = both.y;
-                        }
-#pragma unroll
-                        for (int c = 0; c < 4; c += STEP) acc[n][c] = __fmaf_rn(f[c & 1], sum[n][c], acc[n][c]);
-                    }
-                }
-            }
+            run_products<BF16_X, BF16_S, COUNT, ONE, NT>(acc, ring + slot * STAGE, min((uint32_t)RUN, a.blocks - q * RUN), (q - q0) * RUN, x_lane,
+                                                         factor, g, t);
             slot = slot + 1 == STAGES ? 0 : slot + 1;
             next_slot = next_slot + 1 == STAGES ? 0 : next_slot + 1;
         }
@@ -384,6 +404,93 @@ gemv_w4_kernel(const __grid_constant__ GemvArgs a)
         store_y(a, i / rows, blockIdx.x * rows + i % rows, total);
     }
     cluster.sync();                              // nobody leaves while others read its sums
+}
+
+// The same for up to eight rows of x that shared memory holds whole and many rows of W: one CTA a multiprocessor, which
+// stages x once and takes `tiles` tiles of 16 rows.  Their runs, tile after tile, are one row of work of which each warp takes an
+// equal share, without a pause from tile to tile; a share may begin and end inside a tile.
+template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int STAGES>
+__global__ void __launch_bounds__(STREAM_WARPS * 32, 1)
+gemv_w4_stream_kernel(const __grid_constant__ GemvArgs a, const uint32_t cta_tiles)
+{
+    constexpr int SB = COUNT * (BF16_S ? 2 : 1), COLS = ONE ? 1 : 8, WARPS = STREAM_WARPS;
+    constexpr int STAGE = TILE * (ROW_PITCH + RUN * SB);
+    extern __shared__ __align__(16) unsigned char smem[];
+    const uint32_t lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), g = (int)lane >> 2, t = (int)lane & 3;
+    const uint32_t runs = (a.blocks + RUN - 1) / RUN, tile0 = blockIdx.x * cta_tiles;
+    const uint32_t tiles = min(cta_tiles, (a.n + TILE - 1) / TILE - tile0), items = tiles * runs;
+    const int stride = runs * (RUN * W4_BLOCK) + 32;               // as above
+    unsigned char* ring = smem + warp * (STAGES * STAGE);
+    float* part = reinterpret_cast<float*>(smem);                  // at the end, over the rings: [warp][2][m][TILE]
+    float* factor = reinterpret_cast<float*>(smem + WARPS * STAGES * STAGE);
+    __half* xs = reinterpret_cast<__half*>(factor + (BF16_X ? (runs * RUN * COLS + 3) / 4 * 4 : 0));
+
+    const uint32_t begin = items * warp / WARPS, end = items * (warp + 1) / WARPS;
+    uint32_t tile = begin / runs, q = begin % runs, ahead = begin, ahead_tile = tile, ahead_q = q;      // ahead: what is copied next
+    const StageCopy<SB> copy(a, lane);
+    auto issue = [&](int slot) {
+        if (ahead < end) {
+            const uint32_t row = (tile0 + ahead_tile) * TILE;
+            copy.stage(a, ring + slot * STAGE, a.codes + (uint64_t)row * copy.pitch, a.scales + (uint64_t)row * a.row_scale_bytes, ahead_q,
+                       min((uint32_t)TILE, a.n - row));
+            ++ahead;
+            if (++ahead_q == runs) { ahead_q = 0; ++ahead_tile; }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) issue(s);                 // on their way before x is staged
+    stage_x<BF16_X, COLS, WARPS>(a, 0, runs * RUN, xs, stride, factor);
+    __syncthreads();
+
+    // early: the sums of the tile that the share begins inside, where it ends beyond it
+    float acc[1][4] = {{0.0f, 0.0f, 0.0f, 0.0f}}, early[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const __half* x_lane[1] = {xs + (size_t)(ONE ? 0 : min(g, a.m - 1)) * stride + 8 * t};
+    bool from_start = q == 0;                    // the share holds the tile's first run
+    int slot = 0, next_slot = STAGES - 1;
+    for (uint32_t item = begin; item < end; ++item) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        __syncwarp();                            // this stage has arrived for all lanes, and all have read the one before it
+        issue(next_slot);
+        run_products<BF16_X, BF16_S, COUNT, ONE, 1>(acc, ring + slot * STAGE, min((uint32_t)RUN, a.blocks - q * RUN), q * RUN, x_lane, factor, g, t);
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        next_slot = next_slot + 1 == STAGES ? 0 : next_slot + 1;
+        if (++q == runs) {                       // the tile's last run
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (from_start) store_y(a, 2 * t + (i & 1), (tile0 + tile) * TILE + g + 8 * (i >> 1), acc[0][i]);
+                else early[i] = acc[0][i];
+                acc[0][i] = 0.0f;
+            }
+            q = 0;
+            ++tile;
+            from_start = true;
+        }
+    }
+    // The sums of tiles that warps share, added in the warps' order.  A warp has up to two: of the tile that its share begins
+    // inside and of the one that it ends inside; the former alone if the share lies inside one tile.
+    __syncthreads();                             // the rings have been read
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int col = 2 * t + (i & 1);
+        if (col < a.m) {
+            float* mine = part + (warp * 2 * a.m + col) * TILE + g + 8 * (i >> 1);
+            mine[0] = from_start ? early[i] : acc[0][i];
+            mine[a.m * TILE] = acc[0][i];
+        }
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < tiles * TILE * a.m; i += WARPS * 32) {
+        const uint32_t row = i % TILE, col = i / TILE % a.m, of = i / TILE / a.m;
+        // the warps that hold the tile's first and last run
+        const uint32_t first = ((of * runs + 1) * WARPS - 1) / items, last = ((of + 1) * runs * WARPS - 1) / items;
+        if (first == last) continue;
+        float total = part[((first * 2 + 1) * a.m + col) * TILE + row];
+        for (uint32_t w = first + 1; w <= last; ++w)
+            if (items * w / WARPS != items * (w + 1) / WARPS) total = __fadd_rn(total, part[(w * 2 * a.m + col) * TILE + row]);
+        store_y(a, col, (tile0 + of) * TILE + row, total);
+    }
 }
 
 template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int NT, int STAGES>
@@ -436,10 +543,39 @@ int launch(GemvArgs a, cudaStream_t stream)
     return cudaGetLastError() == cudaSuccess ? FBSR_OK : FBSR_ERR_CUDA;
 }
 
+// Whether the call suits the stream kernel: x fits beside the rings, every multiprocessor has a tile, every warp two runs or
+// more, and no more than a quarter of the warps' time is lost to shares that are a run longer than others.  It stages x once a
+// multiprocessor and has no pause between tiles, the other kernel finer shares: 128000 x 4096 50.6 us against 55.0, with four rows
+// of x 51.8 against 63.0, with eight 58.7 against 75.8; 4096 x 11008 (0.79 of the time filled) 9.0 against 9.9, 14336 x 4096 (0.76)
+// 11.2 against 11.7; 20000 x 2048 (0.70) 9.5 against 9.2, 4096 x 4096 (one run a warp) 6.0 against 5.8.
+template <bool BF16_X, bool BF16_S, int COUNT, bool ONE, int STAGES>
+bool launch_stream(const GemvArgs& a, cudaStream_t stream, int* status)
+{
+    auto kernel = gemv_w4_stream_kernel<BF16_X, BF16_S, COUNT, ONE, STAGES>;
+    constexpr int COLS = ONE ? 1 : 8, STAGE = TILE * (ROW_PITCH + RUN * COUNT * (BF16_S ? 2 : 1)), RINGS = STREAM_WARPS * STAGES * STAGE;
+    constexpr uint32_t SMS = 148, SMEM_CTA = 226 * 1024;
+    static_assert(STREAM_WARPS * 2 * TILE * COLS * 4 <= RINGS, "the partial sums fit over the rings");
+    const uint32_t tiles = (a.n + TILE - 1) / TILE, runs = (a.blocks + RUN - 1) / RUN;
+    const uint64_t bytes = RINGS + (BF16_X ? (uint64_t)runs * RUN * COLS * 4 : 0) + (uint64_t)a.m * (runs * (RUN * W4_BLOCK) + 32) * 2 + 16;
+    if (tiles < SMS || bytes > SMEM_CTA) return false;
+    const uint32_t cta_tiles = (tiles + SMS - 1) / SMS;
+    const uint64_t share = ((uint64_t)cta_tiles * runs + STREAM_WARPS - 1) / STREAM_WARPS;
+    if (share * STREAM_WARPS >= (1u << 27) || share < 2 || (uint64_t)tiles * runs * 4 < share * STREAM_WARPS * SMS * 3) return false;
+    static std::atomic<uint64_t> allowed{0};
+    *status = allow_shared_memory((const void*)kernel, SMEM_CTA, allowed);
+    if (*status != FBSR_OK) return true;
+    kernel<<<(tiles + cta_tiles - 1) / cta_tiles, STREAM_WARPS * 32, bytes, stream>>>(a, cta_tiles);
+    count_launch();
+    *status = cudaGetLastError() == cudaSuccess ? FBSR_OK : FBSR_ERR_CUDA;
+    return true;
+}
 template <bool BF16_X, bool BF16_S, int COUNT>
 int launch_rows(const GemvArgs& a, cudaStream_t stream)
 {
-    if (a.m == 1) return launch<BF16_X, BF16_S, COUNT, true, 1, 3>(a, stream);
+    int status;
+    if (a.m == 1)
+        return launch_stream<BF16_X, BF16_S, COUNT, true, 3>(a, stream, &status) ? status : launch<BF16_X, BF16_S, COUNT, true, 1, 3>(a, stream);
+    if (a.m <= 8 && launch_stream<BF16_X, BF16_S, COUNT, false, 2>(a, stream, &status)) return status;
     if (a.m <= 8) return launch<BF16_X, BF16_S, COUNT, false, 1, 2>(a, stream);
     if (a.m <= 16) return launch<BF16_X, BF16_S, COUNT, false, 2, 2>(a, stream);
     return launch<BF16_X, BF16_S, COUNT, false, 4, 2>(a, stream);

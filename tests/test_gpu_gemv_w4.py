@@ -98,6 +98,32 @@ def test_wide_and_long(m, n, k):
     check(activations(m, k, 2, "bf16"), codes, scales, w, 64, "fp32", "%d %d %d" % (m, n, k))
 
 
+# Shapes of the kernel for many rows of W: tiles of 16 rows spread over 148 CTAs, of which each CTA's runs of 512 columns are cut
+# into sixteen shares; tiles that one warp has, that two have and that all have, a last tile of 4, 11 and 3 rows, a last run of
+# less than 512 columns, and tiles of a single run.
+@pytest.mark.parametrize("m,n,k,x_type,group,scale_fmt", [
+    (1, 9460, 4001, "bf16", 32, "e8m0"), (1, 4731, 8190, "fp16", 128, "bf16"), (1, 9460, 4096, "bf16", 32, "bf16"),
+    (3, 9460, 4001, "fp16", 64, "bf16"), (8, 9460, 4096, "bf16", 64, "bf16"), (5, 75000, 300, "bf16", 32, "e8m0"),
+    (1, 100003, 130, "fp16", 64, "e8m0"), (2, 2368, 16384, "bf16", 128, "e8m0")])
+def test_many_rows_of_w(m, n, k, x_type, group, scale_fmt):
+    codes, scales, w = weights(n, k, 11, group, scale_fmt)
+    x = activations(m, k, 5, x_type)
+    raw, flat = gu.guarded(m * n, torch.float32)
+    flat.view(torch.uint8).fill_(gu.CANARY)
+    out = fbsr.fbsr_gemv_w4(x, codes, scales, group=group, out=flat.view(m, n))
+    torch.cuda.synchronize()
+    xd = x.double().cpu().numpy()
+    want, mass = xd @ w.T, np.abs(xd) @ np.abs(w).T
+    # as in bound(), but all of a row's groups may be one warp's, and up to sixteen sums are joined
+    steps = 2 * 32 + -(-k // 32) + -(-k // 128) + 16
+    inner = steps * 2.0 ** -24 * mass + 2.0 ** -40 * np.abs(xd).max(1, keepdims=True) * np.abs(w).sum(1)[None, :]
+    lim = inner + UNIT["fp32"] * (np.abs(want) + inner) + TINY["fp32"]
+    off = np.abs(out.double().cpu().numpy() - want)
+    assert (off <= lim).all(), "%d off, worst %.2f of the bound" % ((off > lim).sum(), (off / lim).max())
+    assert gu.canaries_intact(raw, m * n, torch.float32)
+    assert torch.equal(fbsr.fbsr_gemv_w4(x, codes, scales, group=group, out_dtype=torch.float32), out)
+
+
 def test_strides_and_alignment():
     codes, scales, w = weights(130, 777, 1)
     for x_type in ("bf16", "fp16"):
