@@ -207,14 +207,15 @@ int fbsr_round_w4(const void* src, int src_fmt, int64_t src_ld, size_t rows, siz
 /* fbsr_gemv_w4 -- the product of activations with a matrix that fbsr_round_w4 has written (the forward product that the
  * quantised weights of Algorithm 1 exist for):  y[i][r] = sum over c < k of x[i][c] value(W[r][c]),
  * value(W[r][c]) = code s.  Each group's products are exact, summed in binary32 and multiplied by s in binary32; groups
- * are added in binary32, in an order that depends on the shapes alone; one rounding to out_fmt at the end.  bfloat16
+ * are added in binary32, in an order that depends on shapes and types alone; one rounding to out_fmt at the end.  bfloat16
  * elements of x below 2^-32 of the largest finite magnitude of their 128 columns are rounded to 2^-40 of it, and scales
  * above 2^100 may overflow before the sum does.  NaN and infinities in x and NaN scales go where the formula takes them.
  *   x        device, m rows of k values of x_fmt (FBSR_BF16 or FBSR_FP16), row i at x + i ldx (elements)
  *   codes, scales, scale_fmt, group   n x k matrix as written by fbsr_round_w4 (its rows x cols); codes 16-byte aligned,
  *            scales aligned to the scales of 128 elements (1 to 8 bytes); codes beyond column k must be zero
  *   y        device, m rows of n values of out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16) at y + i ldy; must not overlap x
- * Meant for few rows: m <= 8 costs what m = 1 does; every 32 rows read the matrix again.  k = 0 gives zeros. */
+ * Meant for few rows: up to 8 share the reading and decoding of W (128000 x 4096: 51 us for one, 59 for eight); every 32
+ * rows read the matrix again.  k = 0 gives zeros. */
 int fbsr_gemv_w4(const void* x, int x_fmt, int64_t ldx, size_t m, const uint8_t* codes, const void* scales, int scale_fmt,
                  int group, size_t n, size_t k, void* y, int out_fmt, int64_t ldy, void* cuda_stream);
 

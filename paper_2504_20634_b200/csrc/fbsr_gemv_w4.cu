@@ -25,7 +25,7 @@
 // Measured, one row of x, groups of 32, on the device, W not in L2: 128000 x 4096 50.6 us = 5.51 TB/s (0.84 of the measured copy
 // rate), 28672 x 8192 27.1 us, 4096 x 11008 (groups of 128) 9.0 us, 4096 x 4096 5.8 us, 1024 x 4096 3.9 us; eight rows by 11008 x
 // 4096 11.9 us, by 128000 x 4096 58.7 us.  What bounds the large ones is the latency of the instructions of 16 warps a
-// multiprocessor (105 registers a thread allow no more), 111 of them for a 16 x 128 block of one row of x, 177 of eight: 24 warps
+// multiprocessor (102 registers a thread allow no more), 104 of them for a 16 x 128 block of one row of x, 131 of eight: 24 warps
 // with half the run, two tiles a warp, bulk copies a row at a time, codes through registers and blocks without the way out
 // between them were not faster.  The small ones are a launch, x's way to shared memory and one memory latency.
 #include <atomic>
