@@ -2,7 +2,7 @@
 // rounded low-precision copy of the weights.  The arithmetic is stated in include/fbsr.h.
 //
 // The tensor table travels as a kernel argument (up to 400 tensors a launch): nothing is uploaded, nothing has to
-// outlive the call, and gradients may lie elsewhere at every step.  A warp owns 1024 consecutive elements of one
+// outlive the call, and gradients may lie elsewhere at every step.  A warp owns up to 1024 consecutive elements of one
 // tensor and finds the tensor by bisection over the table's running tile counts, so that a tensor of one element
 // costs one warp and a tensor of 2^25 elements spreads over the whole GPU.
 #include <cmath>
@@ -37,7 +37,7 @@ struct AdamwHyper {
 
 namespace {
 
-constexpr int TILE = 1024;                       // elements of a warp: 4 rows of 256
+constexpr int TILE = 1024;                       // elements of a warp: 4 rows of 256 (one where there are few, see launch_chunk)
 constexpr int STATE_BLOCK = 256;                 // elements that share a scale of the 8-bit state: one row
 static_assert(STATE_BLOCK == ROW_ELEMS, "a row is a block");
 constexpr int DRAW_WORDS = 4 * (TILE / 8 + 1);   // words of the generator calls that cover a tile, at most
@@ -45,7 +45,7 @@ constexpr int DRAW_WORDS = 4 * (TILE / 8 + 1);   // words of the generator calls
 template <int CAP> struct AdamwTable {
     fbsr_adamw_tensor t[CAP];
     uint32_t first_tile[CAP + 1];
-    uint32_t count;
+    uint32_t count, tile_rows;                   // rows of a warp's tile: 4 or 1
 };
 
 enum { GRAD_FP32, GRAD_BF16, GRAD_FP16 };
@@ -134,13 +134,13 @@ __device__ __forceinline__ void round_row_exact(const float (&y)[8], const uint3
 
 __device__ __forceinline__ uint32_t rotate(uint32_t w, int by) { return __funnelshift_l(w, w, by); }
 
-// The k-bit draws of the weights' rounding for one warp tile: word w of generator call c lies at 4 c + w.
+// The k-bit draws of the weights' rounding for `count` elements of a warp: word w of generator call c lies at 4 c + w.
 // Returns the place of the tile's first element in the first call.
-__device__ __forceinline__ uint32_t fill_draws(uint32_t* words, uint64_t g0, const AdamwHyper& h, int lane)
+__device__ __forceinline__ uint32_t fill_draws(uint32_t* words, uint64_t g0, int count, const AdamwHyper& h, int lane)
 {
     const uint64_t call0 = h.per_call_log2 ? g0 >> h.per_call_log2 : g0 / (uint32_t)h.per_call;
     const uint32_t base = (uint32_t)(g0 - call0 * (uint32_t)h.per_call);
-    const int calls = (int)(base + TILE + h.per_call - 1) / h.per_call;
+    const int calls = (int)(base + count + h.per_call - 1) / h.per_call;
     for (int c = lane; c < calls; c += 32) reinterpret_cast<uint4*>(words)[c] = philox_block(call0 + c, h.k0, h.k1);
     __syncwarp();
     return base;
@@ -405,7 +405,7 @@ adamw_multi_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_con
     __shared__ __align__(16) uint32_t wordbuf[WARPS_PER_CTA][CLS == NEAREST ? 4 : DRAW_WORDS];
     const uint32_t lane = threadIdx.x & 31;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);             // the same for the warp, and known to be
-    const uint32_t tile = blockIdx.x * WARPS_PER_CTA + warp;
+    const uint32_t tile = blockIdx.x * (blockDim.x / 32) + warp;
     if (tile >= tab.first_tile[tab.count]) return;
 
     uint32_t lo = 0, hi = tab.count;             // first_tile[lo] <= tile < first_tile[hi]
@@ -414,9 +414,9 @@ adamw_multi_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_con
         if (tab.first_tile[mid] <= tile) lo = mid; else hi = mid;
     }
     const fbsr_adamw_tensor& t = tab.t[lo];
-    const uint64_t e0 = (uint64_t)(tile - tab.first_tile[lo]) * TILE;
+    const uint64_t e0 = (uint64_t)(tile - tab.first_tile[lo]) * (tab.tile_rows * ROW_ELEMS);
     const uint64_t g0 = t.offset + e0;           // of the stream of draws
-    const int rows = t.n - e0 >= TILE ? TILE / ROW_ELEMS : (int)(t.n - e0 + ROW_ELEMS - 1) / ROW_ELEMS;
+    const int rows = t.n - e0 >= tab.tile_rows * ROW_ELEMS ? (int)tab.tile_rows : (int)(t.n - e0 + ROW_ELEMS - 1) / ROW_ELEMS;
     Place<FMT, BITS, G> at;
     at.set(t, e0);
 
@@ -431,7 +431,7 @@ adamw_multi_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_con
 
     // the generator runs in the shadow of the first loads
     uint32_t draw_base = 0;
-    if (CLS != NEAREST && at.has_lp) draw_base = fill_draws(wordbuf[warp], g0, h, lane);
+    if (CLS != NEAREST && at.has_lp) draw_base = fill_draws(wordbuf[warp], g0, rows * ROW_ELEMS, h, lane);
     const float gs = h.grad_scale ? __ldg(h.grad_scale) : 1.0f;
 
     for (int row = 0; row < rows; ++row) {
@@ -559,32 +559,44 @@ adamw_multi_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_con
     }
 }
 
+// Four rows to a warp share its generator calls and keep its copies ahead of it; where that leaves most of the GPU idle, a warp
+// takes one row, and a CTA four warps.  8-bit state, bfloat16 gradients: 110,000 elements 8.4 us with four rows, 3.9 with one;
+// 0.45 M 8.4 and 5.4; 0.93 M (six tiles a multiprocessor) 8.3 and 8.1; 1.8 M 11.3 and 12.6.  binary32 state: 0.45 M 8.4 and 5.6,
+// 0.93 M 8.4 and 8.8, 1.8 M 10.4 and 12.4.
+constexpr int FEW_TILES = 6 * 148, FEW_WARPS = 4;
+
 template <int FMT, int BITS, int G, int CLS, int CAP>
 int launch_chunk(const fbsr_adamw_tensor* t, size_t count, const AdamwHyper& h, cudaStream_t stream)
 {
     AdamwTable<CAP> tab;
-    tab.count = 0;
     uint64_t tiles = 0;
+    for (size_t i = 0; i < count; ++i) tiles += (t[i].n + TILE - 1) / TILE;
+    const bool few = tiles < FEW_TILES;
+    tab.tile_rows = few ? 1 : TILE / ROW_ELEMS;
+    const uint32_t tile = tab.tile_rows * ROW_ELEMS;
+    tab.count = 0;
+    tiles = 0;
     for (size_t i = 0; i < count; ++i) {
         if (t[i].n == 0) continue;
         tab.t[tab.count] = t[i];
         tab.first_tile[tab.count++] = (uint32_t)tiles;
-        tiles += (t[i].n + TILE - 1) / TILE;
+        tiles += (t[i].n + tile - 1) / tile;
     }
     tab.first_tile[tab.count] = (uint32_t)tiles;
     if (tiles == 0) return FBSR_OK;
-    const unsigned grid = (unsigned)((tiles + WARPS_PER_CTA - 1) / WARPS_PER_CTA);
-    constexpr int BYTES = WARPS_PER_CTA * RING * Stage<BITS, G>::BYTES;
+    const int warps = few ? FEW_WARPS : WARPS_PER_CTA;
+    const unsigned grid = (unsigned)((tiles + warps - 1) / warps);
+    constexpr int WARP_BYTES = RING * Stage<BITS, G>::BYTES;
     auto kernel = adamw_multi_kernel<FMT, BITS, G, CLS, CAP>;
     static std::atomic<uint64_t> allowed{0};
-    if (int rc = allow_shared_memory((const void*)kernel, BYTES, allowed)) return rc;
-    kernel<<<grid, CTA_THREADS, BYTES, stream>>>(tab, h);
+    if (int rc = allow_shared_memory((const void*)kernel, WARPS_PER_CTA * WARP_BYTES, allowed)) return rc;
+    kernel<<<grid, warps * 32, warps * WARP_BYTES, stream>>>(tab, h);
     count_launch();
     return cudaGetLastError() == cudaSuccess ? FBSR_OK : FBSR_ERR_CUDA;
 }
 
 constexpr int CAP_MANY = 400;                    // 72 + 4 bytes a tensor: under the 32,764 bytes of kernel arguments
-constexpr int CAP_FEW = 48;
+constexpr int CAP_FEW = 48;                      // a shorter argument: a call from Python 7.3 us for 48 tensors, 10.7 for 49
 
 template <int FMT, int BITS, int G, int CLS>
 int launch_all(const fbsr_adamw_tensor* t, size_t count, const AdamwHyper& h, cudaStream_t stream)

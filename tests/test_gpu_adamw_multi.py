@@ -325,6 +325,25 @@ def test_many_tensors(count):
     assert np.array_equal(host(lp)[sel], capi.fbsr_round(host(w)[sel], "bf16", "rtne", 1, 0))
 
 
+@pytest.mark.parametrize("bits,grad,misalign", [(32, "fp32", 0), (32, "bf16", 1), (8, "bf16", 0), (8, "fp16", 8), (8, "fp32", 3)])
+@pytest.mark.parametrize("variant,k,lp", [("srf", 4, "bf16"), ("src", 3, "e4m3"), ("srff", 8, "fp16"), ("srf", 5, "bf16"), ("rto", 1, "fp16")])
+def test_one_large_call_is_many_small_ones(bits, grad, misalign, variant, k, lp):
+    """A call over about a million elements gives a warp four rows, a call over half of that one: the same bits."""
+    sizes, names = (1_000_001, 300, 70001, 1025), ("w", "g", "m", "v", "lp", "ms", "vs")
+    t, u = make(sizes, 9, bits, grad, lp, misalign), make(sizes, 9, bits, grad, lp, misalign)
+    fbsr.fbsr_adamw_multi(t["table"], variant, k, 77, **HYPER)
+    half = 500_224                               # a multiple of 256
+    for i, start in enumerate(offsets_of(sizes)):
+        for lo, hi in ((0, half), (half, sizes[i])) if i == 0 else ((0, sizes[i]),):
+            part = {q: [u[q][i][lo // 256:-(-hi // 256)] if q in ("ms", "vs") else u[q][i][lo:hi]] for q in names if u[q]}
+            more = dict(m_scale=part["ms"], v_scale=part["vs"]) if bits == 8 else {}
+            one = fbsr.FbsrAdamwTensors(part["w"], part["g"], part["m"], part["v"], part["lp"], fmt=lp, offsets=[start + lo], **more)
+            fbsr.fbsr_adamw_multi(one, variant, k, 77, **HYPER)
+    for q in names:
+        for a, b in zip(t[q], u[q]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), q
+
+
 def test_without_low_precision_copies_and_with_other_gradients():
     t = make((1000, 10), 3)
     x = fbsr.FbsrAdamwTensors(t["w"], t["g"], t["m"], t["v"], [t["lp"][0], None])
