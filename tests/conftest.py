@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -25,3 +26,11 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def no_garbage_left():
+    """Tensors that a module's caught exceptions keep in reference cycles go with it, not in the middle of a later test that
+    compares what is allocated."""
+    yield
+    gc.collect()
