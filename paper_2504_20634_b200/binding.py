@@ -448,14 +448,19 @@ def _on(device):
 
 
 def _matrix(t, dtypes, what):
-    """(address, leading dimension) of a 2-D CUDA tensor whose rows are contiguous."""
+    """(address, leading dimension) of a 2-D CUDA tensor whose rows are contiguous and apart: a row repeated or overlapped by
+    the next (expand, unfold) has a stride below its length, and is not taken."""
     if t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
         raise TypeError("%s must be a 2-D CUDA tensor of %s" % (what, " or ".join(map(str, dtypes))))
     rows, cols = t.shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise TypeError("%s must have contiguous rows" % what)
-    return t.data_ptr(), (ld if rows > 1 and ld > cols else cols)
+    if rows <= 1:
+        return t.data_ptr(), cols
+    if ld < cols:
+        raise TypeError("%s must have rows that do not overlap: they are %d elements apart and %d long" % (what, ld, cols))
+    return t.data_ptr(), ld
 
 
 def fbsr_w4_padded(cols):

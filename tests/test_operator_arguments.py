@@ -1,0 +1,66 @@
+"""What the binding hands to the C entry points of the operators over many tensors and 4-bit matrices, and what it refuses
+before it gets there (runs without a GPU: host tensors stand in for those of a device)."""
+import random
+
+import pytest
+import torch
+
+
+class OnDevice:
+    """A host tensor that says it lies on a device."""
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2504_20634_b200 import binding, build
+    build.build()
+    return binding
+
+
+def matrix(b, t):
+    return b._matrix(OnDevice(t), (t.dtype,), "x")
+
+
+def test_rows_that_overlap_or_repeat_are_refused(b):
+    x = torch.zeros(64, dtype=torch.bfloat16)
+    for t in (x.expand(8, -1), x.unfold(0, 16, 8), x.unfold(0, 63, 1), x[:1].expand(4, 1), x.as_strided((3, 16), (15, 1))):
+        with pytest.raises(TypeError):
+            matrix(b, t)
+
+
+def test_leading_dimensions(b):
+    x = torch.zeros(12, 100)
+    for t, ld in ((x, 100), (x[::3], 300), (x[:, 7:50], 100), (x[2:3, 5:9], 4), (x[0].expand(1, -1), 100), (x[:0], 100), (x[:, :1], 100),
+                  (x.as_strided((4, 16), (16, 1)), 16), (x[:1, :1].expand(1, 1), 1)):
+        assert matrix(b, t) == (t.data_ptr(), ld), (t.shape, t.stride())
+    for t in (x[:, :0], x[:0, :0], x.as_strided((5, 0), (0, 1))):      # nothing to read, whatever the stride
+        assert matrix(b, t)[1] >= 0
+    with pytest.raises(TypeError):
+        matrix(b, x.t())
+
+
+def test_rows_as_handed_over_end_inside_the_storage(b):
+    rng = random.Random(3)
+    flat = torch.zeros(400)
+    taken = 0
+    for _ in range(3000):
+        rows, cols, ld = rng.randint(1, 9), rng.randint(1, 40), rng.randint(0, 45)
+        if (rows - 1) * ld + cols > flat.numel():
+            continue
+        t = flat.as_strided((rows, cols), (ld, 1))
+        try:
+            address, given = matrix(b, t)
+        except TypeError:
+            assert rows > 1 and ld < cols
+            continue
+        taken += 1
+        assert (address - flat.data_ptr()) // 4 + (rows - 1) * given + cols <= flat.numel()
+        assert rows == 1 or given == ld
+    assert taken > 500
