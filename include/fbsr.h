@@ -349,6 +349,8 @@ int fbsr_qat_adamw_step(void* w8, const void* grad16, float* m, float* v, size_t
  * products and sums of m' and v' are rounded one by one here (no fma), so that plain binary32 arithmetic reproduces codes:
  *     code = FBSR_E4M3(fl(x fl(1 / s))), the same variant and k_bits as the weights; a root above zero whose code came out
  *     as zero takes the smallest code, so that a moment never vanishes under a step that divides by it.
+ * The quotient m' / d of this state may be one unit off where |m'| < 2^-100 or the quotient is subnormal, and a |d| above 2^126
+ * may count as infinite (an eps above it, or a second moment that overflows).
  * Fresh state is all zeros, scales included.  The draws of element J = offset + j for the two states are bits [0, k) and
  * [8, 8 + k) of halfword J mod 8 (low half of word 0 first) of the generator call with counter (J / 8 lo, hi, 1, 0); the
  * weights draw from counters (.., .., 0, 0) as everywhere else.  Stochastic variants need k_bits <= 8 with 8-bit state

@@ -187,8 +187,9 @@ __device__ __forceinline__ float root_in_range(float v)
     return __fmaf_rn(__fmaf_rn(-g, g, v), __fmul_rn(0.5f, y), g);
 }
 
-// m / d for d = 0 (NaN) or 2^-126 <= d <= 2^126 or an infinite d (an overflowing second moment: zero for finite m).  Quotients
-// whose residual m - q d is below binary32's range (m below about 2^-100) may be one unit off.
+// m / d for 2^-126 <= |d|; |d| beyond 2^126 counts as infinite (an overflowing second moment: zero for finite m).  Quotients whose
+// residual m - q d is below binary32's range (|m| below 2^-100, subnormal quotients) may be one unit off.  NaN where d is zero or
+// subnormal, m infinite or the quotient beyond binary32: the step does those again with the general division.
 __device__ __forceinline__ float quotient(float m, float d)
 {
     float y;
@@ -503,6 +504,14 @@ adamw_multi_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_con
             poison = __fmaf_rn(w[c], 0.0f, poison);
         }
         const bool special = poison != poison;
+        if (BITS == 8 && special) {              // rare: out of the fast quotient's range, or special by the formula
+            take_floats(in + St::W, lane, w);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float d = __fadd_rn(__fmul_rn(r[c], h.c2), h.eps);
+                w[c] = __fmaf_rn(h.neg_c1, __fdiv_rn(m[c], d), __fmul_rn(w[c], h.decay));
+            }
+        }
         const int valid = at.valid(0, lane);
         const bool whole = at.vec && valid == 8;
         store_floats(at.w + lane * 8, whole, valid, w);

@@ -35,3 +35,52 @@ def test_repeated_and_overlapping_rows_are_refused_before_a_launch():
     y = fbsr.fbsr_gemv_w4(token.expand(8, -1).contiguous(), codes, scales)
     assert torch.equal(y, y[:1].expand(8, -1))
     assert torch.equal(fbsr.fbsr_gemv_w4(token.expand(1, -1), codes, scales), fbsr.fbsr_gemv_w4(token, codes, scales)[None])
+
+
+def states(w, g, code_m, scale_m, code_v, scale_v):
+    """The table of one tensor with 8-bit state out of numpy arrays, and its tensors."""
+    t = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (w, g, code_m, code_v, scale_m, scale_v)]
+    lp = torch.empty(w.size, dtype=torch.bfloat16, device="cuda")
+    table = fbsr.FbsrAdamwTensors([t[0]], [t[1]], [t[2]], [t[3]], [lp], m_scale=[t[4]], v_scale=[t[5]])
+    return table, t, lp
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-45, 1e-40, 1.17e-38, 2.0 ** -126, 1e-8, -1e-3])
+def test_quotients_of_the_8bit_step_at_the_ends_of_the_range(eps):
+    """Denominators that are zero, subnormal and negative, moments that are infinite and quotients that overflow: the step is
+    the header's, operation by operation, whatever the neighbours are."""
+    f = np.float32
+    n = 256 * 6 + 9
+    rng = np.random.default_rng(1)
+    w = np.full(n, 0.5, f)
+    g = np.zeros(n, f)
+    code_m, code_v = np.zeros(n, np.uint8), np.zeros(n, np.uint8)
+    scale_m, scale_v = np.zeros(7, f), np.zeros(7, f)
+    g[3:700:5] = f(1e-30)                                    # its square underflows, the first moment does not
+    g[256:512:7] = rng.normal(size=37).astype(f) * f(1e-3)
+    code_m[512:768], scale_m[2] = 0x38, f(1e35)              # 1e35 over a zero root
+    code_m[768:1024:3], scale_m[3] = 0x7E, f(1e36)           # 448e36 is beyond binary32: an infinite first moment
+    code_v[768:1024], scale_v[3] = 0x38, f(1.0)
+    code_m[1024:1280:9], scale_m[4] = 0xB8, f(1e-3)
+    code_v[1024:1280], scale_v[4] = 0x38, f(1e-2)
+    g[1300:1310] = 1e-18                                     # roots above zero, below the fast root's range
+    w[1400::2] = -0.0
+    table, t, lp = states(w, g, code_m, scale_m, code_v, scale_v)
+    # c1 is a power of two, c2 and the decay are one: every operation below is rounded as the step's is
+    fbsr.fbsr_adamw_multi(table, "rtne", 1, 0, lr=2.0 ** -10, beta1=0.9, beta2=0.999, eps=eps, weight_decay=0.0, step=10 ** 6)
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        m = f(0.9) * (capi.decode_array("e4m3", code_m) * np.repeat(scale_m, 256)[:n]) + f(1 - 0.9) * g
+        root = capi.decode_array("e4m3", code_v) * np.repeat(scale_v, 256)[:n]
+        v = f(0.999) * (root * root) + (f(1 - 0.999) * g) * g
+        d = np.sqrt(v) + f(eps)
+        want = w - f(2.0 ** -10) * (m / d)
+    assert all(x.dtype == f for x in (m, v, d, want))
+    got = gu.to_np(t[0])
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    assert np.array_equal(got[ok], want[ok]), np.nonzero(got[ok] != want[ok])[0][:5]
+    if eps > 0:
+        assert ok.all() and np.isinf(want[512:768]).any() and np.isinf(want[768:1024]).any()
+    with np.errstate(invalid="ignore"):
+        gu.assert_codes_equal(lp.view(torch.uint16), capi.fbsr_round(got, "bf16", "rtne", 1, 0))
