@@ -177,7 +177,7 @@ round_w4_kernel(const __grid_constant__ RoundW4Args a, const uint64_t first_tile
     auto next = [&] {                            // the place in the tile's next row of 256 elements
         Octet o;
         o.block = block; o.row = row; o.c0 = in_row * W4_BLOCK + place * 8;
-        o.valid = block >= a.blocks ? -1 : min(max((int)(a.cols - o.c0), 0), 8);
+        o.valid = block >= a.blocks ? -1 : (int)min(max(a.cols, o.c0) - o.c0, 8u);      // cols may be 2^31
         // two blocks on; out of the stream before the matrix into its first or second block
         const bool before = (int32_t)block < 0 && first < 0;
         block += 2;

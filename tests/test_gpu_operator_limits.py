@@ -84,3 +84,20 @@ def test_quotients_of_the_8bit_step_at_the_ends_of_the_range(eps):
         assert ok.all() and np.isinf(want[512:768]).any() and np.isinf(want[768:1024]).any()
     with np.errstate(invalid="ignore"):
         gu.assert_codes_equal(lp.view(torch.uint16), capi.fbsr_round(got, "bf16", "rtne", 1, 0))
+
+
+def test_a_row_of_2_to_31_columns():
+    """The largest row: its first and last thousand elements round as they do by themselves, codes, scales and values."""
+    n, part = 1 << 31, 1024
+    x = torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x[0, :part] = torch.randn(part, device="cuda", generator=gen)
+    x[0, -part:] = torch.randn(part, device="cuda", generator=gen)
+    values = torch.full_like(x, 9.0)
+    codes, scales = fbsr.fbsr_round_w4(x, "srf", 4, 5, values=values)
+    for at in (0, n - part):
+        own = torch.empty(1, part, dtype=torch.bfloat16, device="cuda")
+        c, s = fbsr.fbsr_round_w4(x[:, at:at + part].contiguous(), "srf", 4, 5, offset=at, values=own)
+        assert torch.equal(codes[:, at // 2:(at + part) // 2], c) and torch.equal(scales[:, at // 32:(at + part) // 32], s)
+        assert torch.equal(values[:, at:at + part], own)
+    assert not codes[0, part // 2:-part // 2].any() and not values[0, part:-part].any()
