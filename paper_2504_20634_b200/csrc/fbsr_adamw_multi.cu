@@ -659,18 +659,6 @@ namespace {
 typedef int (*launch_fn)(const fbsr_adamw_tensor*, size_t, int, int, AdamwHyper, cudaStream_t);
 const launch_fn kLaunch[5] = {adamw_multi_0, adamw_multi_1, adamw_multi_2, adamw_multi_3, adamw_multi_4};
 
-// beta^step by repeated multiplication, as fbsr_adam_scalars forms it (and stopped where it stops: below 2^-54 the
-// difference to one is one).
-double power(double b, int step)
-{
-    double p = 1.0;
-    for (int t = 0; t < step; ++t) {
-        p *= b;
-        if (std::fabs(b) < 1.0 && std::fabs(p) < 0x1p-54) break;
-    }
-    return p;
-}
-
 inline bool off(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
 }  // namespace
@@ -705,8 +693,9 @@ extern "C" int fbsr_adamw_multi(const fbsr_adamw_tensor* tensors, size_t count, 
     }
     AdamwHyper h{};
     h.beta1 = (float)beta1; h.beta2 = (float)beta2; h.eps = (float)eps;
-    h.neg_c1 = -(float)(lr / (1.0 - power(beta1, step)));
-    h.c2 = (float)(1.0 / std::sqrt(1.0 - power(beta2, step)));
+    // pow and not the products of fbsr_adam_scalars, which cost 53 us at step 100,000 (beta2 0.999; 138 with 0.9999): more than a step
+    h.neg_c1 = -(float)(lr / (1.0 - std::pow(beta1, step)));
+    h.c2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, step)));
     h.a1 = (float)(1.0 - beta1); h.a2 = (float)(1.0 - beta2);
     h.decay = (float)(1.0 - lr * weight_decay);
     h.grad_scale = grad_scale;

@@ -101,3 +101,24 @@ def test_a_row_of_2_to_31_columns():
         assert torch.equal(codes[:, at // 2:(at + part) // 2], c) and torch.equal(scales[:, at // 32:(at + part) // 32], s)
         assert torch.equal(values[:, at:at + part], own)
     assert not codes[0, part // 2:-part // 2].any() and not values[0, part:-part].any()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("step,beta2", [(1, 0.999), (10 ** 4, 0.9999), (10 ** 5, 0.9999), (10 ** 6, 0.999999), (2 ** 31 - 1, 0.9999999)])
+def test_late_steps(bits, step, beta2):
+    """The bias corrections of early and late steps, against binary64."""
+    from test_gpu_adamw_multi import HYPER, make, setup_module as prepare_module, step64, within
+    import test_gpu_adamw_multi
+    prepare_module(test_gpu_adamw_multi)
+    h = dict(HYPER, step=step, beta2=beta2)
+    t = make((70001,), 3, bits=bits)
+    w, g, m, v = (gu.to_np(t[q][0]).copy() for q in ("w", "g", "m", "v"))
+    if bits == 8:
+        rep = lambda s: np.repeat(gu.to_np(s), 256)[:70001]  # noqa: E731
+        m = capi.decode_array("e4m3", m) * rep(t["ms"][0])
+        root = capi.decode_array("e4m3", v) * rep(t["vs"][0])
+        v = root * root
+    fbsr.fbsr_adamw_multi(t["table"], "srf", 4, 1, **h)
+    torch.cuda.synchronize()
+    want, bound = step64(w, g, m, v, h)
+    within(gu.to_np(t["w"][0]), want[0], bound[0], "w")

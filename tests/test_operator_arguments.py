@@ -64,3 +64,25 @@ def test_rows_as_handed_over_end_inside_the_storage(b):
         assert (address - flat.data_ptr()) // 4 + (rows - 1) * given + cols <= flat.numel()
         assert rows == 1 or given == ld
     assert taken > 500
+
+
+def test_the_host_part_of_a_late_step_costs_what_an_early_one_does(b):
+    """beta^step is not formed step by step: 2^31 - 1 products take seconds, and a call launches after them."""
+    import time
+    t = (b.FbsrAdamwTensor * 1)()                            # a tensor without elements: nothing is launched
+    for beta1, beta2 in ((0.9, 1.0 - 2.0 ** -40), (1.0 - 2.0 ** -50, 0.999)):
+        start = time.perf_counter()
+        assert b._L.fbsr_adamw_multi(t, 1, 32, 0x20, 0, 1, 4, 0, 1e-3, beta1, beta2, 1e-8, 0.0, 2 ** 31 - 1, None, None) == 0
+        assert time.perf_counter() - start < 0.2
+
+
+def test_powers_of_beta_give_the_scalars_of_the_single_tensor_step(b):
+    """pow in binary64 and repeated products round to the same binary32 scalars."""
+    import numpy as np
+    f = np.float32
+    steps = list(range(1, 1500)) + [10 ** 4, 12345, 10 ** 5, 10 ** 6]
+    for beta1, beta2 in ((0.9, 0.999), (0.5, 0.95), (0.8, 0.9999), (0.98, 0.99999)):
+        b1, b2, lr = float(f(beta1)), float(f(beta2)), float(f(1e-3))
+        for step in steps:
+            got = b.fbsr_adam_scalars(lr, b1, b2, step)
+            assert got[0] == f(lr / (1 - b1 ** step)) and got[1] == f(1 / np.sqrt(1 - b2 ** step)), (beta1, beta2, step)
