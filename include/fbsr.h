@@ -193,7 +193,8 @@ int fbsr_round_mx(const float* src, void* dst, uint8_t* scales, size_t n, int fm
  *              bits; in every 64 bytes (128 elements) word 4 j + t of plain order lies at place 4 t + j (j, t = 0..3).
  *   scales     device, rows x (padded / group) bytes or bfloat16
  *   values     NULL, or device, rows x cols of src_fmt at values + r values_ld: the values that the codes stand for, rounded
- *              once to src_fmt (what a forward pass over 4-bit weights multiplies with); must not overlap src
+ *              once to src_fmt (what a forward pass over 4-bit weights multiplies with); must not overlap src (src
+ *              itself is refused)
  *   offset     a multiple of 128, at most 2^62; element (r, c) has the global index offset + r padded + c for its draw.
  * At most 2^30 blocks of 128 (FBSR_ERR_TOO_LARGE).  Rows whose addresses allow it (32 bytes for binary32, 16 for 16-bit) are
  * read and written eight elements at a time. */
@@ -213,7 +214,8 @@ int fbsr_round_w4(const void* src, int src_fmt, int64_t src_ld, size_t rows, siz
  *   x        device, m rows of k values of x_fmt (FBSR_BF16 or FBSR_FP16), row i at x + i ldx (elements)
  *   codes, scales, scale_fmt, group   n x k matrix as written by fbsr_round_w4 (its rows x cols); codes 16-byte aligned,
  *            scales aligned to the scales of 128 elements (1 to 8 bytes); codes beyond column k must be zero
- *   y        device, m rows of n values of out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16) at y + i ldy; must not overlap x
+ *   y        device, m rows of n values of out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16) at y + i ldy; must not overlap x (x
+ *            itself is refused)
  * Meant for few rows: up to 8 share the reading and decoding of W (128000 x 4096: 51 us for one, 59 for eight); every 32
  * rows read the matrix again.  k = 0 gives zeros. */
 int fbsr_gemv_w4(const void* x, int x_fmt, int64_t ldx, size_t m, const uint8_t* codes, const void* scales, int scale_fmt,

@@ -623,6 +623,7 @@ extern "C" int fbsr_gemv_w4(const void* x, int x_fmt, int64_t ldx, size_t m, con
     a.out_fmt = out_fmt;
     const launch_fn launch_m = kLaunch[x_fmt == FBSR_BF16][scale_fmt == FBSR_SCALE_BF16][group == 32 ? 0 : group == 64 ? 1 : 2];
     if (off(x, 2) || off(codes, 16) || off(scales, block_scale_bytes)) return FBSR_ERR_ALIGNMENT;
+    if (y == x) return FBSR_ERR_INVALID_ARG;
     for (size_t at = 0; at < m; at += GEMV_MAX_M) {
         a.x = static_cast<const uint16_t*>(x) + (int64_t)at * ldx;
         a.y = static_cast<char*>(y) + (int64_t)at * ldy * (int64_t)out_bytes;

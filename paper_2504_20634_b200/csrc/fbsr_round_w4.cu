@@ -332,6 +332,7 @@ extern "C" int fbsr_round_w4(const void* src, int src_fmt, int64_t src_ld, size_
     if (cols > ((size_t)1 << 31) || rows > ((size_t)1 << 40)) return FBSR_ERR_TOO_LARGE;
     const uint64_t row_blocks = fbsr_w4_padded(cols) / W4_BLOCK;
     if (rows > ((uint64_t)1 << 30) / row_blocks) return FBSR_ERR_TOO_LARGE;         // 2^37 elements
+    if (values == src) return FBSR_ERR_INVALID_ARG;
     RoundW4Args a{};
     a.src = src; a.codes = codes; a.scales = scales; a.values = values;
     a.src_ld = src_ld; a.values_ld = values_ld;

@@ -86,3 +86,11 @@ def test_powers_of_beta_give_the_scalars_of_the_single_tensor_step(b):
         for step in steps:
             got = b.fbsr_adam_scalars(lr, b1, b2, step)
             assert got[0] == f(lr / (1 - b1 ** step)) and got[1] == f(1 / np.sqrt(1 - b2 ** step)), (beta1, beta2, step)
+
+
+def test_results_written_over_their_source_are_refused(b):
+    a, other, invalid = 4096, 8192, 1
+    before = b.fbsr_launch_count()
+    assert b._L.fbsr_round_w4(a, 0x20, 128, 4, 128, other, other, 0, 32, a, 128, 1, 4, 0, 0, None) == invalid       # values on src
+    assert b._L.fbsr_gemv_w4(a, 0, 256, 1, other, other, 0, 32, 16, 256, a, 0x20, 16, None) == invalid               # y on x
+    assert b.fbsr_launch_count() == before
