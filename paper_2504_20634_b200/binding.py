@@ -7,6 +7,7 @@ torch's current stream of the tensors' device.
 """
 import contextlib
 import ctypes
+import itertools
 import os
 
 import torch
@@ -356,7 +357,8 @@ class FbsrAdamwTensors:
     (uint8 or float8_e4m3fn) with m_scale, v_scale (float32, one per 256 elements); lp: the low-precision copies (codes
     of `fmt`, or a tensor of the torch dtype of that format), with None for tensors that have none, or None for all.
     offsets: the tensors' places in the stream of random draws, multiples of 256; by default each tensor starts at the
-    next multiple of 256 after the previous one.  Holds references to the tensors; set_grads() exchanges the gradients."""
+    next multiple of 256 after the previous one.  What a step writes must lie apart.  Holds references to the tensors;
+    set_grads() exchanges the gradients."""
 
     def __init__(self, w, g, m, v, lp=None, fmt="bf16", m_scale=None, v_scale=None, offsets=None):
         count = len(w)
@@ -392,6 +394,9 @@ class FbsrAdamwTensors:
                 d.v_scale = self._pointer(v_scale[i], blocks, (torch.float32,), "v_scale", i)
             d.w_lp = None if lp[i] is None else self._pointer(lp[i], n, code, "lp", i)
             d.n, d.offset = n, int(offsets[i])
+            if d.offset != offsets[i]:
+                raise ValueError("offsets[%d] must be from 0 to 2^64 - 1" % i)
+        self._refuse_overlaps()
         self.set_grads(g)
 
     def _pointer(self, t, n, dtypes, what, i):
@@ -400,6 +405,18 @@ class FbsrAdamwTensors:
         if t.numel() != n:
             raise ValueError("%s[%d] has %d elements, expected %d" % (what, i, t.numel(), n))
         return t.data_ptr()
+
+    def _refuse_overlaps(self):
+        """What a step writes must lie apart: a parameter listed twice would be stepped by two warps at once."""
+        spans = []
+        for t in itertools.chain(self._w, *self._state, self._lp):
+            if t is not None and t.numel():
+                at = t.data_ptr()
+                spans.append((at, at + t.numel() * t.element_size()))
+        spans.sort()
+        for (_, end), (start, _) in zip(spans, spans[1:]):
+            if start < end:
+                raise ValueError("tensors that a step writes overlap, or one is listed twice")
 
     def set_grads(self, g):
         if len(g) != self.count:

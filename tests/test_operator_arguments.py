@@ -94,3 +94,38 @@ def test_results_written_over_their_source_are_refused(b):
     assert b._L.fbsr_round_w4(a, 0x20, 128, 4, 128, other, other, 0, 32, a, 128, 1, 4, 0, 0, None) == invalid       # values on src
     assert b._L.fbsr_gemv_w4(a, 0, 256, 1, other, other, 0, 32, 16, 256, a, 0x20, 16, None) == invalid               # y on x
     assert b.fbsr_launch_count() == before
+
+
+def table(b, w, m=None, v=None, lp=None, **more):
+    like = lambda given: [torch.zeros_like(t) for t in w] if given is None else given  # noqa: E731
+    lists = [[OnDevice(t) for t in x] for x in (w, like(None), like(m), like(v))]
+    return b.FbsrAdamwTensors(*lists, None if lp is None else [t if t is None else OnDevice(t) for t in lp], **more)
+
+
+def test_a_tensor_listed_twice_or_lying_on_another_is_refused(b):
+    flat, other = torch.zeros(1000), torch.zeros(600)
+    apart = [flat[:300], flat[300:600], other, flat[600:600], flat[600:]]
+    table(b, apart)                                          # neighbours and empty tensors are no overlap
+    for w in ([flat, other, flat], [flat, flat], [flat[:301], flat[300:600]], [other, flat[:600], flat[599:]]):
+        with pytest.raises(ValueError):
+            table(b, w)
+    for more in (dict(m=apart), dict(v=apart), dict(lp=[None, flat.view(torch.bfloat16)[:300], None, None, None])):
+        with pytest.raises(ValueError):
+            table(b, apart, **more)
+    # 8-bit state: codes in one buffer behind one another, then scales that two tensors share
+    w, codes, scales = [torch.zeros(300), torch.zeros(500)], torch.zeros(1600, dtype=torch.uint8), torch.zeros(8)
+    part = lambda x, cut: [OnDevice(x[a:e]) for a, e in cut]  # noqa: E731
+    state = [part(codes, ((0, 300), (300, 800))), part(codes, ((800, 1100), (1100, 1600)))]
+    lists = [[OnDevice(t) for t in w], [OnDevice(torch.zeros_like(t)) for t in w], *state]
+    b.FbsrAdamwTensors(*lists, m_scale=part(scales, ((0, 2), (2, 4))), v_scale=part(scales, ((4, 6), (6, 8))))
+    with pytest.raises(ValueError):
+        b.FbsrAdamwTensors(*lists, m_scale=part(scales, ((0, 2), (1, 3))), v_scale=part(scales, ((4, 6), (6, 8))))
+
+
+def test_offsets_outside_the_stream_are_refused(b):
+    w = [torch.zeros(300), torch.zeros(10)]
+    t = table(b, w, offsets=[0, 2 ** 64 - 256])
+    assert t.array[1].offset == 2 ** 64 - 256
+    for offsets in ([-256, 0], [0, 2 ** 64], [0, -2 ** 64]):
+        with pytest.raises(ValueError):
+            table(b, w, offsets=offsets)
