@@ -24,14 +24,6 @@ template <> struct Format<E2M1> {
 constexpr int W4_BLOCK = 128;                    // elements of a block of codes
 constexpr int W4_BLOCK_BYTES = 64;
 
-// Two codes (one byte) to two binary16 values, exact.
-__device__ __forceinline__ uint32_t e2m1_pair_to_half2(uint32_t byte)
-{
-    uint32_t r;
-    asm("{\n\t.reg .b8 b;\n\tcvt.u8.u32 b, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(r) : "r"(byte));
-    return r;
-}
-
 // Eight codes (a word of the stored order) to four pairs of binary16 values.
 __device__ __forceinline__ void e2m1_word_to_half2(uint32_t word, uint32_t (&h)[4])
 {
