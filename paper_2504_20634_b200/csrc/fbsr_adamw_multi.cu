@@ -56,8 +56,10 @@ enum { ADD = 0 /* SRFF, SRF */, PREROUND = 1 /* SRC */, NEAREST = 2 /* the deter
 // ---------------------------------------------------------------------------- rounding with a run-time draw width
 // The row rounder of the bandwidth kernel (round_row_fast) with k as run-time data: the value is rescaled so that the
 // target's exponent range starts where binary32's does, the draw is added where the excess bits end, the code comes out in
-// the top K bits.  It holds while the draw and the half step fit under the 24 - P excess bits of the rescaled pattern
-// (k <= 22 - P, and any k for bfloat16, which is not rescaled; 11 for binary16).
+// the top K bits.  It holds while the draw and the half step fit under the 24 - P excess bits of the rescaled pattern: k <= 22 - P,
+// 14 for bfloat16 and 11 for binary16.  Wider draws round element by element, as the IEEE overflow option does: 62 M parameters,
+// binary32 state, 277 us in the row form, 278 with bfloat16 at k = 16, 285 with IEEE overflow, 310 with binary16 at k = 13; 8-bit
+// state 229, 277 with IEEE overflow.
 template <int FMT> struct Row {
     using F = Format<FMT>;
     static constexpr int SH0 = 24 - F::P, L = FMT == BF16 ? 0 : 31 - (F::K - 1) - SH0;
@@ -177,8 +179,8 @@ __device__ __forceinline__ void take_draws(const uint32_t* words, uint32_t base,
 // of elementary functions on the IBM RISC System/6000 processor", 1990): the compiler's own forms test every operand for
 // special cases, sixteen branches a row, which kept the 8-bit step from overlapping its elements.
 
-// Square root of 2^-96 <= v <= 2^126 (where the residual v - g g is exact), equal to the rounded root for every binary32 number
-// of that range; NaN for NaN.
+// Square root of 2^-96 <= v <= 2^126 (where the residual v - g g is exact); NaN for NaN.  Equal to the rounded root for every number of
+// [1, 4), [2^-96, 2^-94) and [2^124, 2^126), which the tests go through.
 __device__ __forceinline__ float root_in_range(float v)
 {
     float y;
@@ -605,7 +607,7 @@ int launch_chunk(const fbsr_adamw_tensor* t, size_t count, const AdamwHyper& h, 
 }
 
 constexpr int CAP_MANY = 400;                    // 72 + 4 bytes a tensor: under the 32,764 bytes of kernel arguments
-constexpr int CAP_FEW = 48;                      // a shorter argument: a call from Python 7.3 us for 48 tensors, 10.7 for 49
+constexpr int CAP_FEW = 48;                      // with the scalars under 4 KB of argument: a call from Python 7.3 us for 48 tensors, 10.7 for 49
 
 template <int FMT, int BITS, int G, int CLS>
 int launch_all(const fbsr_adamw_tensor* t, size_t count, const AdamwHyper& h, cudaStream_t stream)

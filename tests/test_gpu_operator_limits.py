@@ -122,3 +122,35 @@ def test_late_steps(bits, step, beta2):
     torch.cuda.synchronize()
     want, bound = step64(w, g, m, v, h)
     within(gu.to_np(t["w"][0]), want[0], bound[0], "w")
+
+
+def test_every_root_of_two_binades_as_the_8bit_step_uses_it():
+    """Second moments over all 2^24 numbers of [1, 4), and times 4^-48 and 4^62.  With eps = -2^n the denominator is the root's
+    distance from the lower end of its range, exactly, so that one unit of the root shows in the quotient and in the weight."""
+    f = np.float32
+    target = np.arange(0x3F800000, 0x40800000, dtype=np.uint32).view(f)
+    # v' = fl(fl(V / 2) + fl(fl(g / 2) g)): V the square of a code, the largest with V / 2 below 0.97 of the target, g the rest
+    code = np.arange(0x30, 0x48, dtype=np.uint8)
+    halves = (f(0.5) * capi.decode_array("e4m3", code) ** 2).astype(f)
+    at = np.searchsorted(halves, target.astype(np.float64) * 0.97, side="right") - 1
+    assert at.min() >= 0 and halves[-1] > 4
+    half = halves[at]
+    second = lambda g: half + (f(0.5) * g) * g  # noqa: E731
+    middle = np.sqrt(2.0 * (target.astype(np.float64) - half)).astype(f)
+    g = middle.copy()
+    for step in (-3, -2, -1, 1, 2, 3):
+        other = (middle.view(np.uint32) + np.uint32(step & 0xFFFFFFFF)).view(f)
+        g = np.where((second(g) != target) & (second(other) == target), other, g)
+    reached = second(g) == target
+    assert reached.all()
+    root = np.sqrt(second(g))
+    with np.errstate(divide="ignore"):
+        want = -f(2.0 ** -10) * (g / (root - f(1)))
+    assert want.dtype == f
+    blocks = target.size // 256
+    for n in (0, -48, 62):
+        s = f(2.0 ** n)
+        table, t, _ = states(np.zeros_like(g), g * s, np.zeros(target.size, np.uint8), np.zeros(blocks, f), code[at], np.full(blocks, s))
+        fbsr.fbsr_adamw_multi(table, "rtne", 1, 0, lr=2.0 ** -10, beta1=0.0, beta2=0.5, eps=-2.0 ** n, weight_decay=0.0, step=2000)
+        got = gu.to_np(t[0])
+        assert np.array_equal(got, want), "2^%d: %d of %d differ" % (n, (got != want).sum(), want.size)
