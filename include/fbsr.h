@@ -207,8 +207,9 @@ int fbsr_round_w4(const void* src, int src_fmt, int64_t src_ld, size_t rows, siz
 
 /* fbsr_gemv_w4 -- the product of activations with a matrix that fbsr_round_w4 has written (the forward product that the
  * quantised weights of Algorithm 1 exist for):  y[i][r] = sum over c < k of x[i][c] value(W[r][c]),
- * value(W[r][c]) = code s.  Each group's products are exact, summed in binary32 and multiplied by s in binary32; groups
- * are added in binary32, in an order that depends on shapes and types alone; one rounding to out_fmt at the end.  bfloat16
+ * value(W[r][c]) = code s.  Each group's products are exact, summed in the matrix unit (binary32 sums, which it may truncate where
+ * it aligns their terms: up to 2^-23 a step) and multiplied by s in binary32; groups are added in binary32, in an order that
+ * depends on shapes and types alone; one rounding to out_fmt at the end.  bfloat16
  * elements of x below 2^-32 of the largest finite magnitude of their 128 columns are rounded to 2^-40 of it, and scales
  * above 2^100 may overflow before the sum does.  NaN and infinities in x and NaN scales go where the formula takes them.
  *   x        device, m rows of k values of x_fmt (FBSR_BF16 or FBSR_FP16), row i at x + i ldx (elements)

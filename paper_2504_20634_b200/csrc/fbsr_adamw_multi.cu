@@ -397,7 +397,7 @@ __device__ __forceinline__ void store_floats(float* p, bool whole, int count, co
 
 // Rows of a warp's ring, and resident CTAs the compiler must allow.  62 M parameters, k = 4, bfloat16 copies: binary32 state and
 // gradients 274 us (6.77 TB/s: memory bounds it) with two rows and two or three CTAs; 8-bit state and bfloat16 gradients 212 us
-// (4.69 TB/s: issue slots 84 % busy, 102 instructions an element) with two rows and three CTAs.  Before the last
+// (4.69 TB/s: issue slots 85 % busy, 103 instructions an element) with two rows and three CTAs.  Before the last
 // instructions were saved it was 222, with two CTAs 250 and with three rows 225.
 constexpr int RING = 2, CTAS_32 = 2, CTAS_8 = 3;
 

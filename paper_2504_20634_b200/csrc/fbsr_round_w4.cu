@@ -151,7 +151,8 @@ struct Octet {
 
 // Rows of 256 whose loads are in flight before the first is used, and resident CTAs the compiler must allow: 4096 x 11008
 // binary32 with values, k = 4, took 63 us (6.1 TB/s) with 2 and 4, 73 with 1 and 4, 64 with 4 and 4 or 2 and 5, 70 with three
-// CTAs.  Without values 55 us: then it is the instructions (37 an element) that bound it, not memory.
+// CTAs.  Without values it takes 57 us for 31 us of bytes and from bfloat16 64 us for 31: then it is the instructions that bound it
+// (33 and 38 issue slots an element, 37 with values from binary32; issue 76 to 79 % busy).
 constexpr int W4_BATCH = 2, W4_CTAS = 4;
 
 template <int TYPE, int VAR, int K>
