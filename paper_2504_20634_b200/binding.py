@@ -7,7 +7,6 @@ torch's current stream of the tensors' device.
 """
 import contextlib
 import ctypes
-import itertools
 import os
 
 import torch
@@ -378,45 +377,51 @@ class FbsrAdamwTensors:
             if len(x) != count:
                 raise ValueError("%s has %d entries for %d tensors" % (what, len(x), count))
         self.fmt, self.device = fmt, w[0].device if count else None
+        self._ordinal = w[0].get_device() if count else -1
         self.array = (FbsrAdamwTensor * max(count, 1))()
         self.count = count
         self._w, self._state, self._lp = list(w), (list(m), list(v), list(m_scale), list(v_scale)), list(lp)
         state = (torch.float32,) if self.state_bits == 32 else (torch.uint8, torch.float8_e4m3fn)
         code = (CODE_DTYPE[_fmt_name(fmt)],) + ((VIEW_DTYPE[_fmt_name(fmt)],) if _fmt_name(fmt) in VIEW_DTYPE else ())
+        state_bytes, code_bytes = self.state_bits // 8, code[0].itemsize
+        spans = []                                   # (first byte, last byte + 1) of what a step writes
         for i in range(count):
             n, d = w[i].numel(), self.array[i]
             blocks = -(-n // ADAMW_BLOCK)
-            d.w = self._pointer(w[i], n, (torch.float32,), "w", i)
-            d.m = self._pointer(m[i], n, state, "m", i)
-            d.v = self._pointer(v[i], n, state, "v", i)
+            d.w = at = self._pointer(w[i], n, (torch.float32,), "w", i)
+            spans.append((at, at + 4 * n))
+            d.m = at = self._pointer(m[i], n, state, "m", i)
+            spans.append((at, at + state_bytes * n))
+            d.v = at = self._pointer(v[i], n, state, "v", i)
+            spans.append((at, at + state_bytes * n))
             if self.state_bits == 8:
-                d.m_scale = self._pointer(m_scale[i], blocks, (torch.float32,), "m_scale", i)
-                d.v_scale = self._pointer(v_scale[i], blocks, (torch.float32,), "v_scale", i)
-            d.w_lp = None if lp[i] is None else self._pointer(lp[i], n, code, "lp", i)
-            d.n, d.offset = n, int(offsets[i])
-            if d.offset != offsets[i]:
+                d.m_scale = at = self._pointer(m_scale[i], blocks, (torch.float32,), "m_scale", i)
+                spans.append((at, at + 4 * blocks))
+                d.v_scale = at = self._pointer(v_scale[i], blocks, (torch.float32,), "v_scale", i)
+                spans.append((at, at + 4 * blocks))
+            if lp[i] is not None:
+                d.w_lp = at = self._pointer(lp[i], n, code, "lp", i)
+                spans.append((at, at + code_bytes * n))
+            offset = int(offsets[i])
+            if not 0 <= offset < 1 << 64:
                 raise ValueError("offsets[%d] must be from 0 to 2^64 - 1" % i)
-        self._refuse_overlaps()
+            d.n, d.offset = n, offset
+        # a parameter listed twice would be stepped by two warps at once
+        spans.sort()
+        reach = 0
+        for start, end in spans:
+            if start < reach and start < end:
+                raise ValueError("tensors that a step writes overlap, or one is listed twice")
+            if end > reach:
+                reach = end
         self.set_grads(g)
 
     def _pointer(self, t, n, dtypes, what, i):
-        if not (t.is_cuda and t.device == self.device and t.is_contiguous() and t.dtype in dtypes):
+        if not (t.dtype in dtypes and t.is_cuda and t.get_device() == self._ordinal and t.is_contiguous()):
             raise TypeError("%s[%d] must be a contiguous tensor of %s on %s" % (what, i, " or ".join(map(str, dtypes)), self.device))
         if t.numel() != n:
             raise ValueError("%s[%d] has %d elements, expected %d" % (what, i, t.numel(), n))
         return t.data_ptr()
-
-    def _refuse_overlaps(self):
-        """What a step writes must lie apart: a parameter listed twice would be stepped by two warps at once."""
-        spans = []
-        for t in itertools.chain(self._w, *self._state, self._lp):
-            if t is not None and t.numel():
-                at = t.data_ptr()
-                spans.append((at, at + t.numel() * t.element_size()))
-        spans.sort()
-        for (_, end), (start, _) in zip(spans, spans[1:]):
-            if start < end:
-                raise ValueError("tensors that a step writes overlap, or one is listed twice")
 
     def set_grads(self, g):
         if len(g) != self.count:

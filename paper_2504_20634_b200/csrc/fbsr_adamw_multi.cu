@@ -58,8 +58,8 @@ enum { ADD = 0 /* SRFF, SRF */, PREROUND = 1 /* SRC */, NEAREST = 2 /* the deter
 // target's exponent range starts where binary32's does, the draw is added where the excess bits end, the code comes out in
 // the top K bits.  It holds while the draw and the half step fit under the 24 - P excess bits of the rescaled pattern: k <= 22 - P,
 // 14 for bfloat16 and 11 for binary16.  Wider draws round element by element, as the IEEE overflow option does: 62 M parameters,
-// binary32 state, 277 us in the row form, 278 with bfloat16 at k = 16, 285 with IEEE overflow, 310 with binary16 at k = 13; 8-bit
-// state 229, 277 with IEEE overflow.
+// binary32 state, 277 us in the row form, 279 with bfloat16 at k = 16, 283 with IEEE overflow, 292 with binary16 at k = 13; 8-bit
+// state 219, 276 with IEEE overflow.
 template <int FMT> struct Row {
     using F = Format<FMT>;
     static constexpr int SH0 = 24 - F::P, L = FMT == BF16 ? 0 : 31 - (F::K - 1) - SH0;
