@@ -177,6 +177,9 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, int row_tile, int h
     return w;
 }
 
+// Chunks that a sequence of `length` tokens has, one at least.  Lengths and chunks together may pass 31 bits.
+__device__ __forceinline__ int splits_of(int length, int chunk) { return length > 0 ? (length - 1) / chunk + 1 : 1; }
+
 // The joining kernel may be launched once every CTA has come here; it waits for what they write.
 __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

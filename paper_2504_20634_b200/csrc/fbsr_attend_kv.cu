@@ -419,7 +419,7 @@ attend_kv_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ C
     });
     cluster_barrier();
     constexpr int OCTETS = DIM / 8;
-    const int splits = max((w.length + a.chunk - 1) / a.chunk, 1);
+    const int splits = splits_of(w.length, a.chunk);
 #pragma unroll 1
     for (int i = split * THREADS + threadIdx.x; i < TILE_ROWS * OCTETS; i += splits * THREADS) {
         const int r = i / OCTETS, octet = i % OCTETS, row = w.first_row + r;
@@ -463,7 +463,7 @@ join_few_kernel(const __grid_constant__ AttendArgs a)
     wait_for_kernel_before();
     const int row = w.first_row + threadIdx.x / OCTETS, octet = threadIdx.x % OCTETS;
     if (row >= w.rows) return;
-    const int splits = max((w.length + a.chunk - 1) / a.chunk, 1);
+    const int splits = splits_of(w.length, a.chunk);
     const int qi = row / a.share, heads = a.kv_heads * a.share, head = kv_head * a.share + row - qi * a.share;
     const int64_t at = (int64_t)(w.start + qi) * heads + head, step = (int64_t)a.total * heads;
     float m = LOWEST;
@@ -495,7 +495,7 @@ join_many_kernel(const __grid_constant__ AttendArgs a)
     wait_for_kernel_before();
     const int row = w.first_row, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (row >= w.rows) return;
-    const int splits = max((w.length + a.chunk - 1) / a.chunk, 1);
+    const int splits = splits_of(w.length, a.chunk);
     const int qi = row / a.share, heads = a.kv_heads * a.share, head = kv_head * a.share + row - qi * a.share;
     const int64_t at = (int64_t)(w.start + qi) * heads + head, step = (int64_t)a.total * heads;
     float m = LOWEST;
