@@ -311,8 +311,8 @@ int fbsr_attend_kv(const void* q, int64_t q_token_stride, int64_t q_head_stride,
  *              overlap src (src itself is refused)
  *   offset     a multiple of 128, at most 2^62; element (r, c) has the index J = offset + r padded + c, its draw is bits [0, k) of
  *              halfword J mod 8 (low half of word 0 first) of the generator call with counter (J / 8 lo, hi, 4, 0).
- * At most 2^31 - 1 rows and 2^31 - 256 columns.  Any element alignment is accepted; rows whose addresses are multiples of 32
- * bytes (binary32) or 16 are moved eight elements at a time. */
+ * At most 2^31 - 1 rows and 2^31 - 256 columns.  Without rows or without columns nothing is written, the scales (2^-126 each) neither.
+ * Any element alignment is accepted; rows whose addresses are multiples of 32 bytes (binary32) or 16 are moved eight elements at a time. */
 size_t fbsr_i8_padded(size_t cols);
 int fbsr_round_i8(const void* src, int src_fmt, int64_t src_ld, size_t rows, size_t cols, int8_t* codes, float* scales, void* values,
                   int64_t values_ld, int variant, int k_bits, uint64_t seed, uint64_t offset, void* cuda_stream);

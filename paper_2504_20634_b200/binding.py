@@ -799,6 +799,8 @@ def fbsr_round_i8(src, variant, k_bits, seed, offset=0, values=None, out=None, s
                                   seed, offset, _raw_stream(device))
     if status:
         _check(status, "fbsr_round_i8")
+    if cols == 0:
+        scales.fill_(2.0 ** -126)                # rows without an element: the C entry writes nothing
     return out, scales
 
 
