@@ -134,11 +134,12 @@ __device__ __forceinline__ void write_octet(const RoundI8Args& a, uint64_t row, 
     reinterpret_cast<uint2*>(a.codes)[row * a.octets + octet] = make_uint2(word[0], word[1]);
     if constexpr (VALUES) {
         if (octet * 8 >= a.cols) return;
+        // an integer has one zero: the sum with +0 makes +0 of -0 and changes nothing else
         float v[8];
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             if constexpr (KIND == RULE_EVEN) v[c] = __fmul_rn(__fsub_rn(__uint_as_float(t[c]), 12582912.0f), s.scale);
-            else v[c] = copysignf(__fmul_rn(__fsub_rn(__uint_as_float(t[c] & 0xFFFF0000u), 128.0f), s.scale), __uint_as_float(y[c]));
+            else v[c] = __fmaf_rn(copysignf(__fsub_rn(__uint_as_float(t[c] & 0xFFFF0000u), 128.0f), __uint_as_float(y[c])), s.scale, 0.0f);
         }
         const int valid = (int)min(a.cols - octet * 8, 8u);
         store8<TYPE>(a.values, (int64_t)row * a.values_ld + octet * 8, valid, a.values_whole && valid == 8, v);
