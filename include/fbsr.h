@@ -259,7 +259,7 @@ int fbsr_round_kv(const fbsr_kv_cache* cache, const void* k, int64_t k_token_str
                   int k_bits, uint64_t seed, uint64_t offset, void* cuda_stream);
 
 /* fbsr_read_kv -- rows of a cache as numbers: code s, rounded once to out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16).  A token whose
- * slot is not one of the cache's gives zeros.  k and v as the sources of fbsr_round_kv, overwritten; they must not overlap. */
+ * slot is not one of the cache's gives zeros.  k and v as the sources of fbsr_round_kv, overwritten; rows of k and v must not overlap (refused). */
 int fbsr_read_kv(const fbsr_kv_cache* cache, const int64_t* slots, size_t tokens, void* k, int64_t k_token_stride,
                  int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride, int out_fmt, void* cuda_stream);
 
@@ -284,7 +284,7 @@ int fbsr_read_kv(const fbsr_kv_cache* cache, const int64_t* slots, size_t tokens
  *   tree       NULL, or device, total queries x tree_words uint64; bit j mod 64 of word j / 64 is draft j.
  *              tree_words: (max_queries + 63) / 64 or more
  *   scale      finite, and so is its product with log2(e)
- *   out        device, total queries x heads x dim of q_fmt; must not overlap q (q itself is refused).  Rows that belong to no
+ *   out        device, total queries x heads x dim of q_fmt; no row of it may overlap one of q (refused).  Rows that belong to no
  *              sequence are left as they were.
  *   workspace  device, fbsr_attend_workspace_bytes(...) bytes, 16-byte aligned; contents on entry are ignored.  Calls that may overlap need
  *              workspaces of their own.
@@ -307,8 +307,8 @@ int fbsr_attend_kv(const void* q, int64_t q_token_stride, int64_t q_head_stride,
  *   codes      device, rows x padded bytes, padded = fbsr_i8_padded(cols): cols rounded up to a multiple of 128, the rest
  *              filled with zeros; 16-byte aligned
  *   scales     device, rows binary32 numbers
- *   values     NULL, or device, rows x cols of src_fmt at values + r values_ld: the values, rounded once to src_fmt; must not
- *              overlap src (src itself is refused)
+ *   values     NULL, or device, rows x cols of src_fmt at values + r values_ld: the values, rounded once to src_fmt; no row
+ *              may overlap one of src (refused)
  *   offset     a multiple of 128, at most 2^62; element (r, c) has the index J = offset + r padded + c, its draw is bits [0, k) of
  *              halfword J mod 8 (low half of word 0 first) of the generator call with counter (J / 8 lo, hi, 4, 0).
  * At most 2^31 - 1 rows and 2^31 - 256 columns.  Without rows or without columns nothing is written, the scales (2^-126 each) neither.
@@ -324,7 +324,8 @@ int fbsr_round_i8(const void* src, int src_fmt, int64_t src_ld, size_t rows, siz
  *   a          device, m x k signed bytes, row i at a + i lda; w device, n x k, row r at w + r ldw; both 16-byte aligned, lda and
  *              ldw multiples of 16
  *   k          columns with their padding: a multiple of 16, not 0, less than 131072 (FBSR_ERR_TOO_LARGE beyond: the sum could overflow)
- *   y          device, m rows of n values of out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16) at y + i ldy; must not overlap a or w
+ *   y          device, m rows of n values of out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16) at y + i ldy; no row may overlap one of
+ *              a or w (refused)
  * Up to 4 rows of a (single tokens) are served by a kernel that reads w once; more by the matrix unit. */
 int fbsr_gemm_i8(const int8_t* a, int64_t lda, size_t m, const float* a_scales, const int8_t* w, int64_t ldw, size_t n,
                  const float* w_scales, size_t k, void* y, int out_fmt, int64_t ldy, void* cuda_stream);

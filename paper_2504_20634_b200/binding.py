@@ -670,7 +670,7 @@ def fbsr_round_kv(cache, k, v, slots, variant, k_bits, seed, offset=0):
 
 def fbsr_read_kv(cache, slots, dtype=torch.bfloat16, k=None, v=None):
     """The keys and values at slots (int64) as numbers: (k, v) [tokens, heads, dim] of dtype, or written to the k and v given
-    (whose dtype counts then).  A slot that the cache does not have gives zeros."""
+    (whose dtype counts then; they may lie in one tensor, but no row on another).  A slot that the cache does not have gives zeros."""
     device = cache._ordinal
     tokens = slots.numel()
     if (k is None) != (v is None):
@@ -705,7 +705,8 @@ def fbsr_attend_kv(q, cache, pages, lengths, starts=None, max_queries=None, tree
     max_queries (1 to 256) at least every sequence's number of them; without starts each sequence has total / batch.
     tree: int64 [total] or [total, words], bit j of a query's row says whether it sees the j-th query of its sequence; without
     it each sees those up to itself.  The context before the queries is seen by all.  scale: dim ** -0.5 unless given.
-    out: may be given, strided likewise; rows of no sequence are left as they were.  workspace: a contiguous uint8 tensor of at
+    out: may be given, strided likewise, no row on one of q; rows of no sequence are left as they were (whatever they held, in an
+    out that the call allocates).  workspace: a contiguous uint8 tensor of at
     least fbsr_attend_workspace_bytes bytes; allocated by the call unless given."""
     device = cache._ordinal
     if q.dim() != 3:

@@ -701,9 +701,10 @@ extern "C" int fbsr_attend_kv(const void* q, int64_t q_token_stride, int64_t q_h
     if (tree != nullptr && (tree_words < (int)((max_queries + 63) / 64) || tree_words > 1024)) return FBSR_ERR_INVALID_ARG;
     if (batch == 0 || total == 0) return FBSR_OK;
     if (q == nullptr || out == nullptr || lengths == nullptr || (pages == nullptr && max_pages > 0)) return FBSR_ERR_INVALID_ARG;
-    if (q == out) return FBSR_ERR_INVALID_ARG;
     if (pages_ld < (int64_t)max_pages && batch > 1) return FBSR_ERR_INVALID_ARG;
     if (off(q, 2) || off(out, 2) || off(pages, 4) || off(lengths, 4) || off(starts, 4) || off(tree, 8)) return FBSR_ERR_ALIGNMENT;
+    if (rows_meet(RowSet(q, q_token_stride, q_head_stride, total, (size_t)heads, (size_t)cache->dim, 2),
+                  RowSet(out, out_token_stride, out_head_stride, total, (size_t)heads, (size_t)cache->dim, 2))) return FBSR_ERR_INVALID_ARG;
     const int64_t capacity = (int64_t)max_pages * cache->page;
     const Plan p = plan_of(*cache, batch, heads, max_queries, capacity);
     const size_t need = workspace_bytes_of(p, total, heads, cache->dim);

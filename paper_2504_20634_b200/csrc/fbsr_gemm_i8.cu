@@ -679,12 +679,14 @@ extern "C" int fbsr_gemm_i8(const int8_t* a, int64_t lda, size_t m, const float*
     if (k % 16 != 0 || k == 0) return FBSR_ERR_INVALID_ARG;
     if (k >= 131072 || m > 0x7FFFFFFFu || n > 0x7FFFFFFFu) return FBSR_ERR_TOO_LARGE;
     if (m == 0 || n == 0) return FBSR_OK;
-    if (a == nullptr || w == nullptr || a_scales == nullptr || w_scales == nullptr || y == nullptr || y == a || y == w) return FBSR_ERR_INVALID_ARG;
+    if (a == nullptr || w == nullptr || a_scales == nullptr || w_scales == nullptr || y == nullptr) return FBSR_ERR_INVALID_ARG;
     if (lda < (int64_t)k || ldw < (int64_t)k || ldy < (int64_t)n) return FBSR_ERR_INVALID_ARG;
     if (lda % 16 != 0 || ldw % 16 != 0) return FBSR_ERR_ALIGNMENT;
     const size_t bytes = out_fmt == FBSR_FP32 ? 4 : 2;
     if (off(a, 16) || off(w, 16) || off(a_scales, 4) || off(w_scales, 4) || off(y, bytes)) return FBSR_ERR_ALIGNMENT;
     if (lda >= (int64_t)1 << 40 || ldw >= (int64_t)1 << 40) return FBSR_ERR_TOO_LARGE;          // what a tensor map's stride holds
+    const RowSet result(y, ldy, 0, m, 1, n, bytes);
+    if (rows_meet(RowSet(a, lda, 0, m, 1, k, 1), result) || rows_meet(RowSet(w, ldw, 0, n, 1, k, 1), result)) return FBSR_ERR_INVALID_ARG;
     GemmArgs g{};
     g.a = a; g.w = w; g.a_scales = a_scales; g.w_scales = w_scales; g.y = y;
     g.lda = lda; g.ldw = ldw; g.ldy = ldy;

@@ -1,5 +1,6 @@
 // Host-side plumbing shared by the translation units of libfbsr.so (not part of the public ABI).
 #pragma once
+#include <algorithm>
 #include <atomic>
 #include <cstddef>
 #include <cstdint>
@@ -64,6 +65,71 @@ inline int allow_shared_memory(const void* kernel, int bytes, std::atomic<uint64
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return 4;
     done.fetch_or(bit, std::memory_order_relaxed);
     return 0;
+}
+
+// Rows of `width` bytes in memory, `outer` times `inner` of them; strides in bytes, the outer one not the smaller.
+struct RowSet {
+    typedef __int128 Wide;                       // no product of a stride and a count passes it
+    Wide base, outer_stride, inner_stride, outer, inner, width;
+
+    RowSet(const void* p, int64_t outer_step, int64_t inner_step, size_t outer_count, size_t inner_count, size_t elements, size_t bytes)
+        : base((Wide)reinterpret_cast<uintptr_t>(p)), outer_stride((Wide)outer_step * (int64_t)bytes), inner_stride((Wide)inner_step * (int64_t)bytes),
+          outer(outer_count), inner(inner_count), width((Wide)elements * (int64_t)bytes)
+    {
+        settle(outer_stride, outer);
+        settle(inner_stride, inner);
+        if (outer_stride < inner_stride) { std::swap(outer_stride, inner_stride); std::swap(outer, inner); }
+    }
+
+    Wide reach() const { return (inner - 1) * inner_stride + width; }
+    Wide end() const { return base + (outer - 1) * outer_stride + reach(); }
+
+    // Whether a row meets the bytes [x, x + n).
+    bool meets(Wide x, Wide n) const
+    {
+        Wide first, last, low, high;
+        steps(x - base, n, reach(), outer_stride, outer, first, last);
+        for (; first <= last; ++first) {
+            steps(x - base - first * outer_stride, n, width, inner_stride, inner, low, high);
+            if (low <= high) return true;
+        }
+        return false;
+    }
+
+private:
+    // The same row again, or one alone, is a row without a stride; a negative stride counts from the other end.
+    void settle(Wide& stride, Wide& count)
+    {
+        if (count <= 1 || stride == 0) { count = 1; stride = 0; }
+        if (stride < 0) { base += (count - 1) * stride; stride = -stride; }
+    }
+    static Wide floor_div(Wide a, Wide b) { return a / b - (a % b < 0 ? 1 : 0); }
+    // The steps 0 <= i < count for which [i stride, i stride + reach) meets [x, x + n).
+    static void steps(Wide x, Wide n, Wide reach, Wide stride, Wide count, Wide& first, Wide& last)
+    {
+        if (stride == 0) { first = 0; last = x < reach && x + n > 0 ? 0 : -1; return; }
+        first = std::max<Wide>(floor_div(x - reach, stride) + 1, 0);
+        last = std::min<Wide>(floor_div(x + n - 1, stride), count - 1);
+    }
+};
+
+// Whether a byte of `read` is one of `written`, whose own rows lie apart.  Apart as a whole, as nearly always: a few comparisons.  Rows of the same
+// strides, as those of one buffer are: the rows of both meet as the first of `read` meets the rows of `written` moved by every difference
+// of their places.  Otherwise row by row.
+inline bool rows_meet(const RowSet& read, const RowSet& written)
+{
+    if (read.end() <= written.base || written.end() <= read.base) return false;
+    if (read.outer_stride == written.outer_stride && read.inner_stride == written.inner_stride) {
+        RowSet moved = written;
+        moved.base -= (read.outer - 1) * read.outer_stride + (read.inner - 1) * read.inner_stride;
+        moved.outer += read.outer - 1;
+        moved.inner += read.inner - 1;
+        return moved.meets(read.base, read.width);
+    }
+    for (RowSet::Wide i = 0; i < read.outer; ++i)
+        for (RowSet::Wide j = 0; j < read.inner; ++j)
+            if (written.meets(read.base + i * read.outer_stride + j * read.inner_stride, read.width)) return true;
+    return false;
 }
 
 void count_launch();                         // bumps the counter behind fbsr_launch_count()

@@ -327,7 +327,9 @@ extern "C" int fbsr_read_kv(const fbsr_kv_cache* cache, const int64_t* slots, si
     bool done = false;
     const int status = fill(a, cache, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, out_fmt, tokens, slots, done);
     if (status != FBSR_OK || done) return status;
-    if (k == v) return FBSR_ERR_INVALID_ARG;
+    const size_t bytes = out_fmt == FBSR_FP32 ? 4 : 2, heads = (size_t)cache->heads, dim = (size_t)cache->dim;
+    if (rows_meet(RowSet(k, k_token_stride, k_head_stride, tokens, heads, dim, bytes), RowSet(v, v_token_stride, v_head_stride, tokens, heads, dim, bytes)))
+        return FBSR_ERR_INVALID_ARG;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     launch_type<-1>(a, out_fmt, cache->bits, cache->dim, stream);
     return cudaGetLastError() == cudaSuccess ? FBSR_OK : FBSR_ERR_CUDA;

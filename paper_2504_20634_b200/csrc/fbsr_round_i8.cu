@@ -276,11 +276,13 @@ extern "C" int fbsr_round_i8(const void* src, int src_fmt, int64_t src_ld, size_
     if (src_fmt != FBSR_FP32 && src_fmt != FBSR_BF16 && src_fmt != FBSR_FP16) return FBSR_ERR_UNSUPPORTED;
     if (offset % 128 != 0 || offset > (1ull << 62)) return FBSR_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return FBSR_OK;
-    if (src == nullptr || codes == nullptr || scales == nullptr || values == src) return FBSR_ERR_INVALID_ARG;
+    if (src == nullptr || codes == nullptr || scales == nullptr) return FBSR_ERR_INVALID_ARG;
     if (src_ld < (int64_t)cols || (values != nullptr && values_ld < (int64_t)cols)) return FBSR_ERR_INVALID_ARG;
     const size_t bytes = src_fmt == FBSR_FP32 ? 4 : 2;
     if (off(src, bytes) || off(values, bytes) || off(codes, 16) || off(scales, 4)) return FBSR_ERR_ALIGNMENT;
     if (rows > 0x7FFFFFFFu || cols > 0x7FFFFF00u) return FBSR_ERR_TOO_LARGE;
+    if (values != nullptr && rows_meet(RowSet(src, src_ld, 0, rows, 1, cols, bytes), RowSet(values, values_ld, 0, rows, 1, cols, bytes)))
+        return FBSR_ERR_INVALID_ARG;
     RoundI8Args a{};
     a.src = src; a.codes = codes; a.scales = scales; a.values = values;
     a.src_ld = src_ld; a.values_ld = values_ld;
