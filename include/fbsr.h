@@ -270,7 +270,8 @@ int fbsr_read_kv(const fbsr_kv_cache* cache, const int64_t* slots, size_t tokens
  * query a sequence is ordinary decoding.  Query head h reads head h / (heads / cache heads).  Per query and head
  *     out = sum_t p_t value(v_t) / sum_t p_t,   p_t = exp(scale q . value(k_t))      over the tokens t that it sees;
  * zeros if it sees none.  The products are of binary16 operands with binary32 sums: codes exactly; bfloat16 queries times a power of
- * two for each head (what is below 2^-38 of its largest element loses bits); weights p_t times the scale of v_t rounded to
+ * two for each head (what is below 2^-38 of its largest element loses bits, as do the scores of a row whose largest element times scale
+ * is below 2^-112); weights p_t times the scale of v_t rounded to
  * binary16, the sum of the p_t from binary32 values.  Within a row of the cache, 4-bit groups more than 2^14 below the row's
  * largest scale lose bits, as do rows of v whose scales are below 2^-70.  A NaN that a query sees makes its result NaN; one
  * that it does not see has no influence.

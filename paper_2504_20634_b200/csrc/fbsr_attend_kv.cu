@@ -230,12 +230,12 @@ attend_kv_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ C
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < 2; ++h) {       // both factors first: a sum of products times one of them may be out of range
                     const float ks = BITS == 4 ? kr[g + 8 * h].scale : bf16_value(k_scales[mine[h]]);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
-                        x[n][2 * h] = __fmul_rn(__fmul_rn(x[n][2 * h], to_score[n][0]), ks);
-                        x[n][2 * h + 1] = __fmul_rn(__fmul_rn(x[n][2 * h + 1], to_score[n][1]), ks);
+                        x[n][2 * h] = __fmul_rn(x[n][2 * h], __fmul_rn(to_score[n][0], ks));
+                        x[n][2 * h + 1] = __fmul_rn(x[n][2 * h + 1], __fmul_rn(to_score[n][1], ks));
                     }
                 }
             }

@@ -426,13 +426,13 @@ attend_rows_kv_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
             const float* ks = k_scale[i & 7];
             const float* vs = v_scale[i & 7];
             const float* vl = v_log[i & 7];
-            // two scores an instruction
+            // two scores an instruction; both factors first, since a sum of products times one of them may be out of range
             const uint64_t to_score2 = pair_of(to_score, to_score);
 #pragma unroll
             for (int c = 0; c < TILE; c += 4) {
                 const ulonglong2 k2 = *reinterpret_cast<const ulonglong2*>(ks + c);
-                parts_of(mul2(mul2(pair_of(x[c], x[c + 1]), to_score2), k2.x), x[c], x[c + 1]);
-                parts_of(mul2(mul2(pair_of(x[c + 2], x[c + 3]), to_score2), k2.y), x[c + 2], x[c + 3]);
+                parts_of(mul2(pair_of(x[c], x[c + 1]), mul2(to_score2, k2.x)), x[c], x[c + 1]);
+                parts_of(mul2(pair_of(x[c + 2], x[c + 3]), mul2(to_score2, k2.y)), x[c + 2], x[c + 3]);
             }
             if (masked) {
 #pragma unroll

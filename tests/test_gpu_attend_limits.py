@@ -1,4 +1,4 @@
-"""fbsr_attend_kv at the ends of what it accepts: the longest sequences."""
+"""fbsr_attend_kv at the ends of what it accepts: the longest sequences, and sizes of queries and keys at the ends of their types."""
 import pytest
 import torch
 
@@ -31,3 +31,21 @@ def test_the_longest_sequence(queries, share):
     table[0, -1] = 1
     got = fbsr.fbsr_attend_kv(q, cache, table, torch.tensor([width * page], dtype=torch.int32, device="cuda"), scale=1.0)
     few.compare(got, q, cache, table[:, -1:], [page], [queries], scale=1.0)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("share", [3, 11, 24, 100])
+def test_large_queries_and_small_keys(bits, share):
+    """Queries near the largest bfloat16 number over keys near the smallest scale, with scores of some tens: what turns a sum of products into
+    a score passes 2^100, and is not to be multiplied by the sum before the key's scale."""
+    n, dim, page = 300, 64, 16
+    gen = few.generator(2)
+    k = torch.randn(n, 1, dim, device="cuda", generator=gen) * 2.0 ** -122
+    v = torch.randn(n, 1, dim, device="cuda", generator=gen)
+    width = -(-n // page)
+    cache = fbsr.FbsrKvCache.empty(width, 1, dim, page, bits)
+    fbsr.fbsr_round_kv(cache, k, v, torch.arange(n, device="cuda"), "rtne", 1, 0)
+    table = torch.arange(width, device="cuda").int()[None]
+    q = (torch.randn(1, share, dim, device="cuda", generator=gen) * 2.0 ** 124).bfloat16()
+    got = fbsr.fbsr_attend_kv(q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), scale=1.0)
+    few.compare(got, q, cache, table, [n], [1], scale=1.0)
