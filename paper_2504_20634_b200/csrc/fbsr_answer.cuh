@@ -64,14 +64,6 @@ __device__ __forceinline__ void widen(const Octet8<TYPE>& o, float (&x)[8])
     }
 }
 
-template <int TYPE>
-__device__ __forceinline__ void load8(const void* base, int64_t at, int valid, bool whole, float (&x)[8])
-{
-    Octet8<TYPE> o;
-    load_octet<TYPE>(base, at, valid, whole, o);
-    widen<TYPE>(o, x);
-}
-
 // Eight binary32 values, each rounded once to TYPE.
 template <int TYPE>
 __device__ __forceinline__ void store8(void* base, int64_t at, int valid, bool whole, const float (&v)[8])
@@ -155,8 +147,8 @@ __device__ __forceinline__ uint32_t finite_amax8_pattern(const float (&x)[8])
     return m;
 }
 
-// Quotients by a number known to the host: n / d = (n * mul) >> (32 + shift) for n < 2^31 (Granlund and Montgomery, "Division by
-// invariant integers using multiplication").
+// Quotients by a number known to the host: n / d = (n * mul) >> (31 + shift) for n < 2^31 and d > 1 (Granlund and Montgomery, "Division
+// by invariant integers using multiplication"); d = 1 is handled apart.
 struct Divider { uint32_t mul, shift, d; };
 
 inline Divider divider(uint32_t d)
@@ -206,7 +198,7 @@ inline RoundRule round_rule(int sh0, int l, int variant, int k)
     r.mask_lo = mask; r.mask_hi = mask << 16;
     r.mul = 1u << p; r.rot = (p + 16) & 31;
     if (variant == SRF || variant == RTA) { r.add = p > 0 ? 1u << (p - 1) : 0u; r.half_hi = 0x8000u; }
-    if (rule_kind(variant) == RULE_NEAREST || variant == RTNE) { r.add = ((1u << (r.pos - 1)) - 1u) << l; r.flip = variant == RTO; }
+    if (rule_kind(variant) == RULE_NEAREST) { r.add = ((1u << (r.pos - 1)) - 1u) << l; r.flip = variant == RTO; }
     return r;
 }
 

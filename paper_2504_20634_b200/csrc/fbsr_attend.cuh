@@ -27,7 +27,7 @@ struct AttendArgs {
     float* part_o;                               // [splits][total * heads][dim]
     float2* part_ml;                             // [splits][total * heads]: maximum, sum
     uint64_t pages;
-    int kv_heads, share, page_shift, max_pages, capacity;      // share: query heads of a cache head; capacity: tokens of a table row
+    int kv_heads, share, page_shift, capacity;      // share: query heads of a cache head; capacity: tokens of a table row
     int total, max_queries, row_tiles, splits, chunk, tree_words;     // chunk: tokens of a split, a multiple of TILE
     Divider by_share;
     int q_whole;                                 // addresses of q are multiples of 16 bytes

@@ -721,7 +721,7 @@ extern "C" int fbsr_attend_kv(const void* q, int64_t q_token_stride, int64_t q_h
     a.pages = cache->pages;
     a.kv_heads = cache->heads; a.share = heads / cache->heads; a.by_share = divider((uint32_t)a.share);
     a.q_whole = !off(q, 16) && q_token_stride % 8 == 0 && q_head_stride % 8 == 0;
-    a.page_shift = __builtin_ctz(cache->page); a.max_pages = (int)max_pages; a.capacity = (int)capacity;
+    a.page_shift = __builtin_ctz(cache->page); a.capacity = (int)capacity;
     a.total = (int)total; a.max_queries = (int)max_queries; a.row_tiles = p.row_tiles; a.splits = p.splits; a.chunk = p.chunk;
     a.clustered = p.clustered;
     a.tree_words = tree_words;
