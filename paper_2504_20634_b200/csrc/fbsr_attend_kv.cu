@@ -25,7 +25,7 @@
 //
 // 8 bits, up to 8 rows: bound by memory (131000 tokens of 8 heads of 128, 270 MB: 48 us, 5.6 TB/s).  4 bits: by instructions
 // (unpacking, scales of groups): the same tokens take 47 us for half the bytes (53 when every lane made the scales that it needs itself).
-#include <cstring>
+#include <cmath>
 
 #include "fbsr_attend.cuh"
 
@@ -545,8 +545,13 @@ struct Plan { int nr, copies, row_tiles, splits, chunk, clustered; };
 // and shared memory hold) with up to eight where there are several sequences or few bytes a token (32 sequences of 1 to 8192 tokens: 61
 // us against 67; one of 131000 in 4 bits: 47 against 51, but in 8 bits 51 against 48); one with the kernels of many rows, whose start
 // and end cost as much as ten tiles.  Several sequences differ in length and leave some of their CTAs without tokens: with few rows
-// three times as many (four times: 64 us, twice: 71), and with many two chunks rather than one where 1.3 times the places hold them (6
-// sequences of 8 heads and two tiles of rows, lengths spread evenly: 49 us with two chunks, 60 with one, 94 with five).  Not shorter
+// three times as many (32 sequences of 1 to 8192 tokens: 64 us with four times, 71 with twice; four models, 4 to 128 sequences of up to 2048, 8192 and
+// 32768 tokens, from all lengths to nearly equal ones: once to six times are within 7 % of one another in the mean, once is better for
+// lengths that are alike and four times for those that are not), and with many two chunks rather than one although the places do not hold them, as long as
+// what the second round of CTAs starts and ends is little beside a chunk: up to a number of (sequence, head, tile of rows) that grows
+// with the table, the line on which both choices cross.  Times of two chunks over those of one, geometric means over 32 to 252 rows and lengths
+// spread from an eighth or a half of the longest: tables of 2048 tokens 0.98 with 80 of them and 1.20 with 88, 3000: 0.92 with 88 and 1.08
+// with 96, 4096: 0.97 with 96 and 1.14 with 104, 8192: 0.90 with 112 and 1.08 with 120; 1024: 1.17 with 80.  Not shorter
 // than MIN_CHUNK tokens.  With few rows, where the cache is what is read, writing and reading a chunk's sums (8 dim bytes a row) should
 // not pass a tenth of reading its tokens: there they are made longer, but not so long that the GPU is no longer full.  (Cutting by the
 // lengths themselves, in the kernel, took longer: every CTA reads them all, and many more have nothing to do.)
@@ -570,7 +575,7 @@ Plan plan_of(const fbsr_kv_cache& c, size_t batch, int heads, size_t max_queries
     const int64_t full = (capacity * units + resident - 1) / resident;
     int64_t pieces = resident / units;
     if (batch > 1 && !p.copies) pieces = 3 * resident / units;
-    else if (batch > 1 && pieces < 2) pieces = 13 * resident / (10 * units);
+    else if (batch > 1 && pieces < 2 && units <= resident && units <= resident * (0.55 + 0.118 * std::log2(capacity / 2048.0))) pieces = 2;
     pieces = pieces < 1 ? 1 : pieces;
     int64_t chunk = (capacity + pieces - 1) / pieces;
     const int64_t worth = p.copies ? 0 : used * c.dim * 8 * 10 / (2 * c.dim * c.bits / 8), longer = worth < full ? worth : full;
