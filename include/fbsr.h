@@ -283,14 +283,14 @@ int fbsr_read_kv(const fbsr_kv_cache* cache, const int64_t* slots, size_t tokens
  *              NULL: every sequence has max_queries of them, one after another.
  *   max_queries  1..256, at least every sequence's number of queries; more are not computed
  *   tree       NULL, or device, total queries x tree_words uint64; bit j mod 64 of word j / 64 is draft j.
- *              tree_words: (max_queries + 63) / 64 or more
+ *              tree_words: (max_queries + 63) / 64 or more, 1024 at most
  *   scale      finite, and so is its product with log2(e)
  *   out        device, total queries x heads x dim of q_fmt; no row of it may overlap one of q (refused).  Rows that belong to no
  *              sequence are left as they were.
  *   workspace  device, fbsr_attend_workspace_bytes(...) bytes, 16-byte aligned; contents on entry are ignored.  Calls that may overlap need
  *              workspaces of their own.
  * An index that is not one of the cache's pages, or a length beyond max_pages pages, makes the results that depend on it NaN;
- * nothing outside the buffers is read.  heads a multiple of the cache's; at most 2^31 - 1 queries, 2^40 rows of them (queries x
+ * nothing outside the buffers is read.  heads a multiple of the cache's; at most 65536 heads, 2^31 - 1 queries, 2^40 rows of them (queries x
  * heads) and 2^31 - 64 tokens a sequence (FBSR_ERR_TOO_LARGE).  The order of summation depends on the arguments, shapes and lengths alone. */
 size_t fbsr_attend_workspace_bytes(const fbsr_kv_cache* cache, size_t batch, size_t total, int heads, size_t max_queries, size_t max_pages);
 int fbsr_attend_kv(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_fmt, size_t total, int heads,
@@ -323,7 +323,7 @@ int fbsr_round_i8(const void* src, int src_fmt, int64_t src_ld, size_t rows, siz
  * the sum exact in 32-bit integers, its conversion to binary32 rounded to nearest.  The bits do not depend on how a product is
  * split into calls.  NaN scales make their rows (columns) of y NaN.
  *   a          device, m x k signed bytes, row i at a + i lda; w device, n x k, row r at w + r ldw; both 16-byte aligned, lda and
- *              ldw multiples of 16
+ *              ldw multiples of 16 below 2^40
  *   k          columns with their padding: a multiple of 16, not 0, less than 131072 (FBSR_ERR_TOO_LARGE beyond: the sum could overflow)
  *   y          device, m rows of n values of out_fmt (FBSR_FP32, FBSR_BF16 or FBSR_FP16) at y + i ldy; no row may overlap one of
  *              a or w (refused)

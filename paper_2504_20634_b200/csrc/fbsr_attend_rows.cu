@@ -23,7 +23,8 @@
 // What bounds it.  A tile of 64 tokens of dim 128 takes 1350 clocks with 128 rows (the softmax of two warps a scheduler: 512 for the
 // exponentials, the rest for their instructions and waits), 870 with 24 (the products need 440; a warp that issues both kinds
 // needs 1000).  Start and end of a CTA take 7 us.  65536 tokens of 8 heads in 8 bits with 128 rows: 52 us, of which the products are 20.7 and
-// the bytes 20.9; 131000 tokens of 4 heads with 40 rows: 42 us of 20.9.
+// the bytes 20.9; 131000 tokens of 4 heads with 40 rows: 40 us, and 45 with the joining, of 20.9.  No unit is saturated: issue slots 59 and 57 %, the
+// product unit 38 and 51 %, the exponential unit 39 and 27 %, memory 34 and 46 %.
 //
 // Scales and weights are as in fbsr_attend_kv.cu; a row's maximum moves only when a weight would pass 2^15, and then the row of O is
 // read, scaled and written back by its thread.
@@ -258,7 +259,7 @@ attend_rows_kv_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
                 __syncwarp();
             };
             // One warp spends 1000 clocks on a tile's waits and products.  With copies that bounds the tile, and each product has a warp
-            // (131000 tokens, 40 rows, 8 bits: 42 us against 47); without, the softmax does, and scores that run ahead of the sums
+            // (131000 tokens, 40 rows, 8 bits: 45 us against 51); without, the softmax does, and scores that run ahead of the sums
             // delay it (128 rows: 55 us against 53): the sums follow two tiles behind the scores in one warp.
             if (warp == PRODUCT_WARP) {
                 for (int i = 0; i < tiles && fine; ++i) {
