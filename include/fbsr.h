@@ -273,8 +273,8 @@ int fbsr_read_kv(const fbsr_kv_cache* cache, const int64_t* slots, size_t tokens
  * two for each head (what is below 2^-38 of its largest element loses bits, as do the scores of a row whose largest element times scale
  * is below 2^-112); weights p_t times the scale of v_t rounded to
  * binary16, the sum of the p_t from binary32 values.  Within a row of the cache, 4-bit groups more than 2^14 below the row's
- * largest scale lose bits, as do rows of v whose scales are below 2^-70.  A NaN that a query sees makes its result NaN; one
- * that it does not see has no influence.
+ * largest scale lose bits, as do rows of v whose scales are below 2^-70; a weight below 2^-134 of the largest product of a weight and its
+ * token's scale of v counts as zero.  A NaN that a query sees makes its result NaN; one that it does not see has no influence.
  *   q          device, total queries x heads x dim of q_fmt (FBSR_BF16 or FBSR_FP16), strides in elements
  *   cache      as above, codes as fbsr_round_kv writes them (no NaN codes) in every slot below a sequence's length
  *   pages      device, batch rows of max_pages page indices (int32), row b at pages + b pages_ld (max_pages or more)
